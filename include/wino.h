@@ -392,6 +392,106 @@ int wino_flex_backward(const wino_conv_desc_t* d, const wino_flex_matrices_t* f,
                        const wino_scales_t* s, void* dx, void* dw, const wino_flex_grads_t* grads,
                        void* workspace, size_t ws_bytes, void* hip_stream);
 
+/* ---- Operators of a training step around the layers ------------------------
+ * Between two layers, behind the last one and behind wino_backward's dw: layer
+ * norm over the channels, the loss of a linear classifier, and the
+ * orthogonalised update made of a weight gradient.  Real tensors are fp32 or
+ * bf16 (WINO_TYPE_*), rows of elements a stride apart (0 = dense, the row's own
+ * length; outputs without a stride are dense).  They may start at any element; 16-byte
+ * aligned tensors with rows of whole 16-byte vectors run fastest.  Outputs must
+ * not overlap inputs or the workspace.  All sums are fp32 or wider and taken in
+ * a fixed order: results are reproducible, bit for bit.  Workspaces are 256-byte
+ * aligned (EWORKSPACE); two calls that may overlap in time need one each. */
+enum { WINO_TYPE_F32 = 0, WINO_TYPE_BF16 = 1, WINO_TYPE_I8 = 2 };
+
+/* Layer norm over the channels of each row (a pixel of an NHWC tensor):
+ *   mu = sum_c x / C,  s = 1 / sqrt(sum_c (x - mu)^2 / C + eps),
+ *   y = (x - mu) s gamma + beta
+ * y_type WINO_TYPE_I8: codes clamp(rint(y / s_y), -127, 127), ties to even, the
+ * int8 input of a layer with s_x = s_y; computed in 64 bits, so that a code is
+ * the formula's (a NaN gives 0).  gamma, beta [C] fp32 (null: ones, zeros);
+ * mean = mu, rstd = s [rows] fp32 outputs for the backward pass, may be null. */
+typedef struct {
+  int64_t rows;
+  int channels;              /* 1 ... 2^24                                      */
+  int x_type, y_type;        /* y_type: also WINO_TYPE_I8                       */
+  int g_type;                /* of dy and dx                                    */
+  float eps, s_y;            /* s_y: read for WINO_TYPE_I8 only                 */
+  int64_t x_stride, y_stride, dy_stride, dx_stride;
+} wino_norm_desc_t;
+int wino_layer_norm(const wino_norm_desc_t* d, const void* x, const void* gamma, const void* beta,
+                    void* y, void* mean, void* rstd, void* hip_stream);
+/* Its gradients, with xh = (x - mean) rstd and g = dy gamma:
+ *   dx = rstd (g - mean_c(g) - xh mean_c(g xh)),
+ *   dgamma = sum_rows dy xh,  dbeta = sum_rows dy
+ * (the cast to int8 codes straight-through, as in wino_backward).  mean, rstd:
+ * the forward pass's.  dgamma, dbeta [C] fp32; each of the three outputs may be
+ * null.  Without rows dgamma and dbeta are zeros.  The workspace (needed for
+ * dgamma, dbeta) holds partial sums. */
+int wino_layer_norm_backward_workspace_bytes(const wino_norm_desc_t* d, size_t* bytes);
+int wino_layer_norm_backward(const wino_norm_desc_t* d, const void* dy, const void* x,
+                             const void* gamma, const void* mean, const void* rstd, void* dx,
+                             void* dgamma, void* dbeta, void* workspace, size_t ws_bytes,
+                             void* hip_stream);
+
+/* Softmax cross entropy of a linear classifier over many classes:
+ *   l = h w^T + bias,  lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t[target_t]
+ * h [rows][features], w [classes][features], bias [classes] fp32 or null,
+ * targets [rows] int64, loss and lse [rows] fp32.  The logits are never kept:
+ * they are computed in pieces and computed again in the backward pass.  A row
+ * whose target is ignore_index or no class (below 0, classes or above) is left
+ * out: loss 0, no gradient, whatever h holds there; its lse is still that of h.  Classes may
+ * be masked by a bias of -infinity: a masked target's loss is +infinity; a row
+ * with every class masked has lse -infinity, loss +infinity and no gradient.
+ * Products of fp32 operands keep 24 bits of each factor. */
+enum { WINO_LOSS_MAX_ROWS = 1 << 21, WINO_LOSS_MAX_FEATURES = 1 << 20, WINO_LOSS_MAX_CLASSES = 1 << 27 };
+typedef struct {
+  int rows, features, classes;
+  int type;                  /* of h, w, dh, dw                                 */
+  int64_t h_stride, w_stride;
+  int64_t ignore_index;
+  int piece;                 /* classes per piece, 0 = chosen by the library (about
+                                256 MiB of workspace); at most WINO_LOSS_MAX_ROWS */
+} wino_loss_desc_t;
+int wino_linear_cross_entropy_workspace_bytes(const wino_loss_desc_t* d, size_t* bytes);
+int wino_linear_cross_entropy(const wino_loss_desc_t* d, const void* h, const void* w,
+                              const void* bias, const void* targets, void* loss, void* lse,
+                              void* workspace, size_t ws_bytes, void* hip_stream);
+/* Its gradients for dloss [rows] fp32, the gradient at each row's loss (1/n for
+ * the mean over n rows), and lse as the forward pass returned it:
+ *   dl_tv = (exp(l_tv - lse_t) - [v = target_t]) dloss_t,
+ *   dh = dl w,  dw = dl^T h,  dbias = sum_t dl
+ * dh [rows][features] and dw [classes][features] dense, of `type`; dbias
+ * [classes] fp32; each may be null.  bf16: dl / max|dloss| is rounded to bf16
+ * before the two products (dbias sums it unrounded).  Without rows dw and dbias
+ * are zeros. */
+int wino_linear_cross_entropy_backward_workspace_bytes(const wino_loss_desc_t* d, size_t* bytes);
+int wino_linear_cross_entropy_backward(const wino_loss_desc_t* d, const void* h, const void* w,
+                                       const void* bias, const void* targets, const void* lse,
+                                       const void* dloss, void* dh, void* dw, void* dbias,
+                                       void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* Orthogonalised update of a weight gradient by Newton-Schulz products (dw
+ * [K][C][3][3] is a matrix of K rows and 9 C columns), `batch` matrices of one
+ * shape at once:
+ *   X = g / (|g|_F + eps);  `steps` times  A = X X^T,  X <- a X + (b A + c A A) X;
+ *   o = scale X
+ * with X taken across where rows > cols.  The products keep 24 bits of each
+ * factor where o is fp32, 16 where it is bf16.  A matrix of zeros gives zeros,
+ * one with a NaN or an infinity NaN. */
+enum { WINO_ORTHOGONALISE_MAX_SIDE = 1 << 20 };
+typedef struct {
+  int batch, rows, cols;     /* batch at most 65535                             */
+  int g_type, o_type;
+  int steps;                 /* 1 ... 100                                       */
+  float a, b, c, eps, scale; /* eps > 0                                         */
+  int64_t g_batch, g_stride; /* elements between matrices (0: rows * stride)    */
+  int64_t o_batch, o_stride; /* and between rows (0: cols)                      */
+} wino_orthogonalise_desc_t;
+int wino_orthogonalise_workspace_bytes(const wino_orthogonalise_desc_t* d, size_t* bytes);
+int wino_orthogonalise(const wino_orthogonalise_desc_t* d, const void* g, void* o, void* workspace,
+                       size_t ws_bytes, void* hip_stream);
+
 /* Measurement helper: the kernel launches wino_conv2d makes for this descriptor,
  * in order, as a comma-separated list written to the host buffer `buf`
  * (NUL-terminated; 128 bytes are always enough).  Names: weight_transform,

@@ -16,4 +16,9 @@ from .binding import (  # noqa: F401
     wino_flex_output_transform, wino_flex_weight_transform, wino_input_transform,
     wino_make_matrices, wino_output_transform, wino_probe_peak, wino_profile_next_launch,
     wino_transform_operands, wino_weight_transform, wino_workspace_bytes,
+    TYPE_BF16, TYPE_F32, TYPE_I8, LossDesc, NormDesc, OrthogonaliseDesc,
+    wino_layer_norm, wino_layer_norm_backward, wino_layer_norm_backward_workspace_bytes,
+    wino_linear_cross_entropy, wino_linear_cross_entropy_backward,
+    wino_linear_cross_entropy_backward_workspace_bytes, wino_linear_cross_entropy_workspace_bytes,
+    wino_orthogonalise, wino_orthogonalise_workspace_bytes,
 )

@@ -9,6 +9,7 @@ BASE_CANONICAL, BASE_LEGENDRE, BASE_CHEBYSHEV, BASE_HERMITE = 0, 1, 2, 3
 OUT_F32, OUT_I32, OUT_I8 = 0, 1, 2
 FUSED_OFF, FUSED_ON, FUSED_AUTO = 0, 1, 2
 LAYOUT_ROWS, LAYOUT_FRAGMENTS = 0, 1
+TYPE_F32, TYPE_BF16, TYPE_I8 = 0, 1, 2
 MAT_NAMES = ("G", "BT", "AT", "PT", "PINVT", "GP", "BPT", "APT")
 EXPORTS = ("wino_make_matrices", "wino_free_matrices", "wino_get_matrix", "wino_get_int_form",
            "wino_workspace_bytes", "wino_operand_bytes", "wino_preferred_operand_layout",
@@ -20,6 +21,11 @@ EXPORTS = ("wino_make_matrices", "wino_free_matrices", "wino_get_matrix", "wino_
            "wino_flex_output_transform", "wino_flex_conv2d", "wino_flex_calibrate",
            "wino_backward_workspace_bytes", "wino_backward_dv_parts", "wino_backward",
            "wino_flex_backward_workspace_bytes", "wino_flex_backward",
+           "wino_layer_norm", "wino_layer_norm_backward_workspace_bytes", "wino_layer_norm_backward",
+           "wino_linear_cross_entropy_workspace_bytes", "wino_linear_cross_entropy",
+           "wino_linear_cross_entropy_backward_workspace_bytes",
+           "wino_linear_cross_entropy_backward", "wino_orthogonalise_workspace_bytes",
+           "wino_orthogonalise",
            "wino_profile_next_launch", "wino_probe_peak", "wino_last_error")
 
 
@@ -109,6 +115,42 @@ class FlexGrads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("dGP", "dBPT", "dAPT")]
 
 
+class NormDesc(C.Structure):
+    """Mirror of wino_norm_desc_t."""
+    _fields_ = ([("rows", C.c_int64)] + [(n, C.c_int) for n in ("channels", "x_type", "y_type", "g_type")] +
+                [("eps", C.c_float), ("s_y", C.c_float)] +
+                [(n, C.c_int64) for n in ("x_stride", "y_stride", "dy_stride", "dx_stride")])
+
+    def __init__(self, rows, channels, x_type=TYPE_F32, y_type=TYPE_F32, g_type=TYPE_F32, eps=1e-5,
+                 s_y=1.0, x_stride=0, y_stride=0, dy_stride=0, dx_stride=0):
+        super().__init__(rows, channels, x_type, y_type, g_type, eps, s_y, x_stride, y_stride,
+                         dy_stride, dx_stride)
+
+
+class LossDesc(C.Structure):
+    """Mirror of wino_loss_desc_t."""
+    _fields_ = ([(n, C.c_int) for n in ("rows", "features", "classes", "type")] +
+                [(n, C.c_int64) for n in ("h_stride", "w_stride", "ignore_index")] +
+                [("piece", C.c_int)])
+
+    def __init__(self, rows, features, classes, type=TYPE_F32, h_stride=0, w_stride=0,
+                 ignore_index=-100, piece=0):
+        super().__init__(rows, features, classes, type, h_stride, w_stride, ignore_index, piece)
+
+
+class OrthogonaliseDesc(C.Structure):
+    """Mirror of wino_orthogonalise_desc_t."""
+    _fields_ = ([(n, C.c_int) for n in ("batch", "rows", "cols", "g_type", "o_type", "steps")] +
+                [(n, C.c_float) for n in ("a", "b", "c", "eps", "scale")] +
+                [(n, C.c_int64) for n in ("g_batch", "g_stride", "o_batch", "o_stride")])
+
+    def __init__(self, batch, rows, cols, g_type=TYPE_F32, o_type=TYPE_F32, steps=5, a=3.4445,
+                 b=-4.7750, c=2.0315, eps=1e-7, scale=1.0, g_batch=0, g_stride=0, o_batch=0,
+                 o_stride=0):
+        super().__init__(batch, rows, cols, g_type, o_type, steps, a, b, c, eps, scale, g_batch,
+                         g_stride, o_batch, o_stride)
+
+
 def lib_path():
     return os.path.join(HERE, "libwino.so")
 
@@ -170,6 +212,17 @@ def _load():
     lib.wino_flex_backward_workspace_bytes.argtypes = [dp, C.POINTER(C.c_size_t)]
     lib.wino_flex_backward.argtypes = [dp, fp, vp, vp, vp, vp, vp, vp, sp, vp, vp,
                                        C.POINTER(FlexGrads), vp, C.c_size_t, vp]
+    npd, lpd, opd = C.POINTER(NormDesc), C.POINTER(LossDesc), C.POINTER(OrthogonaliseDesc)
+    zp = C.POINTER(C.c_size_t)
+    lib.wino_layer_norm.argtypes = [npd] + [vp] * 7
+    lib.wino_layer_norm_backward_workspace_bytes.argtypes = [npd, zp]
+    lib.wino_layer_norm_backward.argtypes = [npd] + [vp] * 9 + [C.c_size_t, vp]
+    lib.wino_linear_cross_entropy_workspace_bytes.argtypes = [lpd, zp]
+    lib.wino_linear_cross_entropy.argtypes = [lpd] + [vp] * 7 + [C.c_size_t, vp]
+    lib.wino_linear_cross_entropy_backward_workspace_bytes.argtypes = [lpd, zp]
+    lib.wino_linear_cross_entropy_backward.argtypes = [lpd] + [vp] * 10 + [C.c_size_t, vp]
+    lib.wino_orthogonalise_workspace_bytes.argtypes = [opd, zp]
+    lib.wino_orthogonalise.argtypes = [opd, vp, vp, vp, C.c_size_t, vp]
     lib.wino_probe_peak.argtypes = [C.c_int, C.c_int, C.c_int, vp, C.POINTER(C.c_double), vp]
     _lib = lib
     return lib
@@ -470,3 +523,70 @@ def wino_flex_calibrate(desc, fm, x, w, y, s_x, s_w, workspace, stream=None):
                                        workspace.numel() * workspace.element_size(),
                                        _stream(stream)))
     return sc
+
+
+def _bytes_of(function, desc):
+    out = C.c_size_t()
+    _check(function(C.byref(desc), C.byref(out)))
+    return out.value
+
+
+def _room(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def wino_layer_norm(desc, x, gamma, beta, y, mean=None, rstd=None, stream=None):
+    """Layer norm of the rows of ``x``; gamma, beta, mean and rstd may be None."""
+    _check(_load().wino_layer_norm(C.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y),
+                                   _ptr(mean), _ptr(rstd), _stream(stream)))
+    return y
+
+
+def wino_layer_norm_backward_workspace_bytes(desc):
+    return _bytes_of(_load().wino_layer_norm_backward_workspace_bytes, desc)
+
+
+def wino_layer_norm_backward(desc, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace,
+                             stream=None):
+    """Gradients of wino_layer_norm; each of dx, dgamma and dbeta may be None."""
+    _check(_load().wino_layer_norm_backward(C.byref(desc), _ptr(dy), _ptr(x), _ptr(gamma),
+                                            _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma),
+                                            _ptr(dbeta), _ptr(workspace), _room(workspace),
+                                            _stream(stream)))
+    return dx, dgamma, dbeta
+
+
+def wino_linear_cross_entropy_workspace_bytes(desc):
+    return _bytes_of(_load().wino_linear_cross_entropy_workspace_bytes, desc)
+
+
+def wino_linear_cross_entropy(desc, h, w, bias, targets, loss, lse, workspace, stream=None):
+    """Loss and log-sum-exp of every row; bias may be None, targets are int64."""
+    _check(_load().wino_linear_cross_entropy(C.byref(desc), _ptr(h), _ptr(w), _ptr(bias),
+                                             _ptr(targets), _ptr(loss), _ptr(lse), _ptr(workspace),
+                                             _room(workspace), _stream(stream)))
+    return loss, lse
+
+
+def wino_linear_cross_entropy_backward_workspace_bytes(desc):
+    return _bytes_of(_load().wino_linear_cross_entropy_backward_workspace_bytes, desc)
+
+
+def wino_linear_cross_entropy_backward(desc, h, w, bias, targets, lse, dloss, dh, dw, dbias,
+                                       workspace, stream=None):
+    """Gradients of wino_linear_cross_entropy; each of dh, dw and dbias may be None."""
+    _check(_load().wino_linear_cross_entropy_backward(
+        C.byref(desc), _ptr(h), _ptr(w), _ptr(bias), _ptr(targets), _ptr(lse), _ptr(dloss),
+        _ptr(dh), _ptr(dw), _ptr(dbias), _ptr(workspace), _room(workspace), _stream(stream)))
+    return dh, dw, dbias
+
+
+def wino_orthogonalise_workspace_bytes(desc):
+    return _bytes_of(_load().wino_orthogonalise_workspace_bytes, desc)
+
+
+def wino_orthogonalise(desc, g, o, workspace, stream=None):
+    """Orthogonalised updates of a batch of weight gradients."""
+    _check(_load().wino_orthogonalise(C.byref(desc), _ptr(g), _ptr(o), _ptr(workspace),
+                                      _room(workspace), _stream(stream)))
+    return o

@@ -21,8 +21,8 @@ HIP_SOURCES = ["wino_kernels.hip", "wino_transforms_f2.hip", "wino_transforms_f4
                "wino_calibrate_f2.hip", "wino_calibrate_f4.hip", "wino_calibrate_f6.hip",
                "wino_flex_f2.hip", "wino_flex_f4.hip", "wino_flex_f6.hip",
                "wino_backward.hip", "wino_flex_backward_f2.hip", "wino_flex_backward_f4.hip",
-               "wino_flex_backward_f6.hip"]
-CXX_SOURCES = ["wino_api.cpp"]
+               "wino_flex_backward_f6.hip", "wino_norm.hip", "wino_loss.hip", "wino_update.hip"]
+CXX_SOURCES = ["wino_api.cpp", "wino_train.cpp"]
 
 COMMON = ["-std=c++20", "-fPIC", "-fconstexpr-steps=200000000", "-Wall", "-Wno-unused-function"]
 # -ffp-contract=off: the only fused multiply-adds are the ones written out (the

@@ -1,0 +1,63 @@
+// Launchers of the operators of a training step (wino_norm.hip, wino_loss.hip, wino_update.hip)
+// behind the entry points in wino_train.cpp.  Not part of the public boundary.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+namespace wino {
+
+inline size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
+
+// ---- layer norm ------------------------------------------------------------------------------
+struct NormArgs {
+  long rows;
+  int channels, x_type, y_type, g_type;
+  float eps, s_y;
+  long x_stride, y_stride, dy_stride, dx_stride;
+};
+hipError_t launch_norm(const NormArgs& a, const void* x, const float* gamma, const float* beta, void* y,
+                       float* mean, float* rstd, hipStream_t st);
+// Work groups of the backward kernel, each with one partial sum of dgamma and of dbeta.
+int norm_parts(long rows, int channels);
+hipError_t launch_norm_backward(const NormArgs& a, const void* dy, const void* x, const float* gamma,
+                                const float* mean, const float* rstd, void* dx, float* dgamma,
+                                float* dbeta, float* parts, hipStream_t st);
+
+// ---- linear cross entropy --------------------------------------------------------------------
+struct LossArgs {
+  int rows, features, classes;
+  int bf16;               // operands and gradients: 0 fp32, 1 bf16
+  long h_stride, w_stride;
+  long ignore_index;
+  int piece;              // classes per piece (0: chosen here)
+};
+// Regions of the workspace, bytes from its start; `bytes` in all.
+struct LossLayout {
+  int planes;             // bf16 planes of an operand
+  int piece, dp, tp;      // classes per piece; features, rows rounded up to whole stages
+  int splits;             // of the classes of a piece in dh's product
+  size_t w, h, parts, target, ref, ht, wt, dl, dlt, dh, dbias, bytes;
+};
+LossLayout loss_layout(const LossArgs& a, bool backward);
+hipError_t launch_loss(const LossArgs& a, const void* h, const void* w, const float* bias,
+                       const int64_t* target, float* loss, float* lse, char* ws, hipStream_t st);
+hipError_t launch_loss_backward(const LossArgs& a, const void* h, const void* w, const float* bias,
+                                const int64_t* target, const float* lse, const float* dloss, void* dh,
+                                void* dw, float* dbias, char* ws, hipStream_t st);
+
+// ---- orthogonalised updates ------------------------------------------------------------------
+struct UpdateArgs {
+  int batch, rows, cols, g_bf16, o_bf16, steps;
+  float a, b, c, eps, scale;
+  long g_batch, g_stride, o_batch, o_stride;
+};
+struct UpdateLayout {
+  int planes, r, c, rp, cp;   // r <= c: the smaller and the larger side; rounded up to whole stages
+  size_t norms, x, xt, x2, xt2, gram, poly, bytes;
+};
+UpdateLayout update_layout(const UpdateArgs& a);
+hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, hipStream_t st);
+
+}  // namespace wino
