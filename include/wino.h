@@ -476,9 +476,10 @@ int wino_linear_cross_entropy_backward(const wino_loss_desc_t* d, const void* h,
  * shape at once:
  *   X = g / (|g|_F + eps);  `steps` times  A = X X^T,  X <- a X + (b A + c A A) X;
  *   o = scale X
- * with X taken across where rows > cols.  The products keep 24 bits of each
- * factor where o is fp32, 16 where it is bf16.  A matrix of zeros gives zeros,
- * one with a NaN or an infinity NaN. */
+ * with X taken across where rows > cols.  The products take 22 bits of each
+ * factor (entries below 2^-18 of the largest possible one: 2^-40 of that) and
+ * sum in fp32.  A matrix of zeros gives zeros, one with a NaN or an infinity
+ * NaN. */
 enum { WINO_ORTHOGONALISE_MAX_SIDE = 1 << 20 };
 typedef struct {
   int batch, rows, cols;     /* batch at most 65535                             */

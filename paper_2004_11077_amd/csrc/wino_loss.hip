@@ -128,7 +128,7 @@ template <class T>
 __global__ __launch_bounds__(T::THREADS) void k_loss_logits(Operand w, Operand h, Logits g, int tiles_m,
                                                             int tiles_n, int part0, float2* __restrict__ best,
                                                             float* __restrict__ hit) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * T::STAGE];
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
   tile_of(tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
                                                              uint16_t* __restrict__ dl, long dl_ld, long dl_plane,
                                                              uint16_t* __restrict__ dlt, long dlt_ld,
                                                              long dlt_plane, float* __restrict__ dbias) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * T::STAGE];
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
   tile_of(tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
@@ -325,7 +325,7 @@ struct Product {
 template <class T>
 __global__ __launch_bounds__(T::THREADS) void k_loss_product(Operand a, Operand b, Product p, int tiles_m,
                                                              int tiles_n) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * T::STAGE];
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
   tile_of(tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
@@ -378,7 +378,7 @@ unsigned grid_of(long items) {
 }
 
 template <int NP>
-using TileFor = Tile<128, 128, 2, 2, NP>;
+using TileFor = Tile<128, 128, 2, 2, NP, NP == 1 ? 4 : 3>;
 constexpr int kBM = 128, kBN = 128, kWN = 2;
 
 // bf16 rows that the products can take where they lie: whole stages of features, 16-byte accesses.

@@ -54,8 +54,9 @@ struct UpdateArgs {
   long g_batch, g_stride, o_batch, o_stride;
 };
 struct UpdateLayout {
-  int planes, r, c, rp, cp;   // r <= c: the smaller and the larger side; rounded up to whole stages
-  size_t norms, x, xt, x2, xt2, gram, poly, bytes;
+  int r, c, rp, cp;           // r <= c: the smaller and the larger side; rounded up to whole blocks of k
+  int splits;                 // ranges of k of A's product
+  size_t norms, x, xt, x2, xt2, gram, poly, parts, bytes;
 };
 UpdateLayout update_layout(const UpdateArgs& a);
 hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, hipStream_t st);

@@ -3,12 +3,17 @@
 //   X = G / (|G|_F + eps);  `steps` times  A = X X^T,  X <- a X + (b A + c A A) X;  O = scale X
 //
 // on the smaller side's products (a taller matrix is taken across).  Three products a step, each with
-// its k contiguous in both operands (wino_products.hpp): A from X, the polynomial a I + b A + c A A from
-// A, which is symmetric, and the new X from the polynomial and X across.  Every product therefore leaves
-// its result cut into planes, the new X both ways.  The step multiplies small singular values by a, an
-// error of an early step with them: fp32 results take three planes (24 bits), bf16 results two (16
-// bits, which after the amplification by 3.4^4 of the usual coefficients still lies below their
-// rounding).
+// its k contiguous in both operands (wino_products.hpp): A from X, the polynomial P = a I + b A + c A A
+// from A, which is symmetric, and the new X from P and X across.  Every product leaves its result cut
+// into the two fp16 planes that the next one takes, blocked as the instruction reads them, the new X
+// both ways.  A step multiplies small singular values by a and the errors of earlier steps with them,
+// by 3.4^4 in all for the usual coefficients, so bf16 results need the second plane as well.
+//
+// Powers of two that bring X, A and P into fp16's range are known on the host: no singular value of X
+// exceeds one at first, nor, after a step, the largest |a s + b s^3 + c s^5| of those before it, and no
+// entry exceeds the largest singular value.  (2^15 is half of what fp16 holds.)
+#include <cmath>
+
 #include "wino_products.hpp"
 #include "wino_train.hpp"
 
@@ -41,17 +46,44 @@ __global__ __launch_bounds__(256) void k_update_norm(const void* __restrict__ g,
   if (threadIdx.x == 0) norms[blockIdx.y * kNormParts + blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// Planes of X, both ways.
+// fp16 planes of a matrix, blocked: rows of kb blocks of 32; 2^e times the values.
 struct Planes {
-  uint16_t *x, *xt;
-  long x_ld, x_plane, x_batch, xt_ld, xt_plane, xt_batch;
+  uint16_t* p;
+  long plane, batch;
+  int kb, e;
 };
 
-// G -> X: 64 x 64 values a work group.
-template <int NP>
+__device__ __forceinline__ float power(int e) { return __builtin_ldexpf(1.f, e); }
+
+// Four consecutive k of a row, from a multiple of four.
+__device__ __forceinline__ void put(const Planes& o, int row, int k, f32x4 v) {
+  uint16_t* to = o.p + blockIdx.z * o.batch + blocked(row, k, o.kb);
+  const float s = power(o.e);
+  uint16_t q[4][2];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) cut<2>(v[e] * s, q[e]);
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+    *reinterpret_cast<ushort4*>(to + p * o.plane) = make_ushort4(q[0][p], q[1][p], q[2][p], q[3][p]);
+}
+// The same four values as one k of four consecutive rows, from a multiple of four.
+__device__ __forceinline__ void put_across(const Planes& o, int row, int k, int rows, f32x4 v) {
+  uint16_t* to = o.p + blockIdx.z * o.batch + blocked(row, k, o.kb);
+  const float s = power(o.e);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (row + e >= rows) continue;
+    uint16_t q[2];
+    cut<2>(v[e] * s, q);
+    to[e * 8] = q[0];
+    to[o.plane + e * 8] = q[1];
+  }
+}
+
+// G -> X, both ways: 64 x 64 values a work group.
 __global__ __launch_bounds__(256) void k_update_planes(const void* __restrict__ g, UpdateArgs a, int r, int c,
-                                                       int across, const double* __restrict__ norms,
-                                                       Planes p) {
+                                                       int across, const double* __restrict__ norms, Planes x,
+                                                       Planes xt) {
   __shared__ float tile[64][65];
   __shared__ double total;
   if (threadIdx.x < 64) {
@@ -63,207 +95,360 @@ __global__ __launch_bounds__(256) void k_update_planes(const void* __restrict__ 
   __syncthreads();
   const double inv = 1.0 / (__builtin_sqrt(total) + (double)a.eps);
   const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;   // of X
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll 4
   for (int i = 0; i < 16; ++i) {
     // lanes along the rows of G
-    const int q = y + i * 4, rr = across ? r0 + x : r0 + q, cc = across ? c0 + q : c0 + x;
+    const int q = wave + i * 4, rr = across ? r0 + lane : r0 + q, cc = across ? c0 + q : c0 + lane;
     float v = 0;
     if (rr < r && cc < c) {
       const long at = blockIdx.z * a.g_batch + (across ? (long)cc * a.g_stride + rr : (long)rr * a.g_stride + cc);
       v = (float)((double)value(g, at, a.g_bf16) * inv);
     }
-    if (across) tile[x][q] = v;
-    else tile[q][x] = v;
+    if (across) tile[lane][q] = v;
+    else tile[q][lane] = v;
   }
   __syncthreads();
-  const int row = threadIdx.x >> 2, eight = (threadIdx.x & 3) * 16;
+  // 16 blocks of 16 x 32, eight of X and eight of X across; a lane's eight values are one store
 #pragma unroll
-  for (int way = 0; way < 2; ++way) {
-    const int first = way ? c0 : r0, rows = way ? c : r;
-    if (first + row >= rows) continue;
+  for (int i = 0; i < 4; ++i) {
+    const int block = wave + i * 4, way = block >> 3, q = block & 7;
+    const int row = (q >> 1) * 16 + (lane & 15), k = (q & 1) * 32 + (lane >> 4) * 8;
+    const Planes& o = way ? xt : x;
+    const int row_at = (way ? c0 : r0) + row, k_at = (way ? r0 : c0) + k;
+    if ((row_at & ~15) >= (way ? c : r) || k_at >= o.kb * 32) continue;
+    const float s = power(o.e);
+    __attribute__((aligned(16))) uint16_t out[2][8];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      __attribute__((aligned(16))) uint16_t out[NP][8];
-      const int at = eight + half * 8;
+    for (int e = 0; e < 8; ++e) {
+      uint16_t h[2];
+      cut<2>((way ? tile[k + e][row] : tile[row][k + e]) * s, h);
+      out[0][e] = h[0];
+      out[1][e] = h[1];
+    }
+    uint16_t* to = o.p + blockIdx.z * o.batch + blocked(row_at, k_at, o.kb);
+    *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(out[0]);
+    *reinterpret_cast<uint4*>(to + o.plane) = *reinterpret_cast<const uint4*>(out[1]);
+  }
+}
+
+// What becomes of the products.  kGram: A.  kPoly: P.  kNext: X both ways.  kLast: the result.
+enum Kind { kGram, kPoly, kNext, kLast };
+struct Result {
+  Planes out, out_t;      // kGram, kPoly: out; kNext: X and X across
+  Planes gram;            // kPoly: A
+  int r, c;               // sides of X
+  int e;                  // exponents of the two operands, added
+  float a, b, c2, scale;
+  int across, bf16;       // kLast
+  void* o;
+  long o_batch, o_stride;
+};
+
+// Four values D[m .. m + 3][n] of a product of batch blockIdx.z: m is a row of the first operand and
+// becomes k of the result's row n.  kGram, kPoly: `mirror` writes row m, k n as well.  Elements of k
+// beyond the matrix, up to whole blocks, become zeros: the next product multiplies them.
+template <Kind KIND>
+__device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, bool mirror) {
+  const float unit = power(-s.e);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint16_t q[NP];
-        cut<NP>(way ? tile[at + e][row] : tile[row][at + e], q);
+  for (int e = 0; e < 4; ++e) v[e] *= unit;
+  const int km = KIND <= kPoly ? s.r : s.c;   // rows of the first operand
+  if constexpr (KIND == kPoly) {
+    if (n < s.r && m < s.gram.kb * 32) {
+      const uint16_t* at = s.gram.p + blockIdx.z * s.gram.batch + blocked(n, m, s.gram.kb);
+      const ushort4 h = *reinterpret_cast<const ushort4*>(at), l = *reinterpret_cast<const ushort4*>(at + s.gram.plane);
+      const float one = power(-s.gram.e);
+      const float old[4] = {f16_value(h.x) + f16_value(l.x), f16_value(h.y) + f16_value(l.y),
+                            f16_value(h.z) + f16_value(l.z), f16_value(h.w) + f16_value(l.w)};
 #pragma unroll
-        for (int n = 0; n < NP; ++n) out[n][e] = q[n];
-      }
+      for (int e = 0; e < 4; ++e)
+        v[e] = __builtin_fmaf(s.c2, v[e], s.b * (old[e] * one)) + (m + e == n ? s.a : 0.f);
+    }
+  }
+  if constexpr (KIND == kLast) {
+    if (n >= s.r) return;
 #pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        uint16_t* to = way ? p.xt + n * p.xt_plane + blockIdx.z * p.xt_batch + (long)(c0 + row) * p.xt_ld + r0 + at
-                           : p.x + n * p.x_plane + blockIdx.z * p.x_batch + (long)(r0 + row) * p.x_ld + c0 + at;
-        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(out[n]);
-      }
+    for (int e = 0; e < 4; ++e) {
+      if (m + e >= s.c) continue;
+      const long at = blockIdx.z * s.o_batch + (s.across ? (long)(m + e) * s.o_stride + n : (long)n * s.o_stride + m + e);
+      if (s.bf16) static_cast<uint16_t*>(s.o)[at] = bf16_bits(s.scale * v[e]);
+      else static_cast<float*>(s.o)[at] = s.scale * v[e];
+    }
+  } else {
+    f32x4 k = v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (m + e >= km) k[e] = 0;
+    if (n < s.r && m < s.out.kb * 32) put(s.out, n, m, k);
+    if (KIND == kNext || mirror) {
+      const Planes& t = KIND == kNext ? s.out_t : s.out;
+      if (n >= s.r) v = f32x4{0, 0, 0, 0};
+      if (n < t.kb * 32) put_across(t, m, n, km, v);
     }
   }
 }
 
-// Four values of a row of planes, from element m.
-template <int NP>
-__device__ __forceinline__ void put(uint16_t* to, long plane, const float (&v)[4]) {
-  uint16_t q[4][NP];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) cut<NP>(v[e], q[e]);
-#pragma unroll
-  for (int p = 0; p < NP; ++p)
-    *reinterpret_cast<ushort4*>(to + p * plane) = make_ushort4(q[0][p], q[1][p], q[2][p], q[3][p]);
+// Tile of a symmetric result: the i-th with its rows' tile not behind its columns'.
+__device__ __forceinline__ void triangle(int i, int& m, int& n) {
+  m = (int)((__builtin_sqrtf(8.f * i + 1.f) - 1.f) * 0.5f);
+  while ((m + 1) * (m + 2) / 2 <= i) ++m;
+  while (m * (m + 1) / 2 > i) --m;
+  n = i - m * (m + 1) / 2;
 }
 
-// One symmetric result [r][rp] on planes.
-struct Symmetric {
-  uint16_t* out;
-  long ld, plane, batch;
-  int r;
-};
-
-// poly = 0: A = X X^T.  poly = 1: a I + b A + c A A from A.
-template <class T, bool POLY>
-__global__ __launch_bounds__(T::THREADS) void k_update_symmetric(Operand x, Symmetric s, int k, int tiles,
-                                                                 float a, float b, float c) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * T::STAGE];
-  const int m0 = blockIdx.x % tiles * T::BM, n0 = blockIdx.x / tiles * T::BN;
+// Products of many tiles.  blockIdx.x: tile, .y: range of k, .z: batch.  With several ranges their fp32
+// sums go to `parts` [range][batch][n][m], for k_update_join.
+template <class T, Kind KIND>
+__global__ __launch_bounds__(T::THREADS) void k_update_product(Operand x, Operand y, int k, int per, int tiles_m,
+                                                               Result s, float* __restrict__ parts, long part,
+                                                               int part_ld) {
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+  int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
+  if constexpr (KIND <= kPoly) triangle(blockIdx.x, tm, tn);
+  const int m0 = tm * T::BM, n0 = tn * T::BN;
+  const int k0 = blockIdx.y * per, k1 = k0 + per < k ? k0 + per : k;
   f32x4 acc[T::TM][T::TN] = {};
-  multiply<T>(x, x, blockIdx.z, m0, n0, 0, k, k, lds, acc);
+  multiply<T>(x, y, blockIdx.z, m0, n0, k0, k1, k, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
 #pragma unroll
   for (int j = 0; j < T::TN; ++j) {
     const int n = n0 + (wn * T::TN + j) * 16 + (lane & 15);
-    if (n >= s.r) continue;
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
       const int m = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4;
-      if (m >= s.ld) continue;
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
-      if constexpr (POLY) {
-        float old[4] = {};
-#pragma unroll
-        for (int p = T::NP - 1; p >= 0; --p) {
-          const ushort4 q = *reinterpret_cast<const ushort4*>(x.p + p * x.plane + blockIdx.z * x.batch + (long)n * x.ld + m);
-          old[0] += bf16_value(q.x), old[1] += bf16_value(q.y), old[2] += bf16_value(q.z), old[3] += bf16_value(q.w);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(c, v[e], b * old[e]) + (m + e == n ? a : 0.f);
-      }
-      put<T::NP>(s.out + blockIdx.z * s.batch + (long)n * s.ld + m, s.plane, v);
-    }
-  }
-}
-
-// New X, both ways; the last step leaves the result instead.
-template <class T, bool LAST>
-__global__ __launch_bounds__(T::THREADS) void k_update_next(Operand xt, Operand poly, Planes p, int k,
-                                                            int tiles_m, UpdateArgs u, int across, void* o) {
-  __shared__ __attribute__((aligned(1024))) char lds[2 * T::STAGE];
-  const int m0 = blockIdx.x % tiles_m * T::BM, n0 = blockIdx.x / tiles_m * T::BN;
-  f32x4 acc[T::TM][T::TN] = {};
-  multiply<T>(xt, poly, blockIdx.z, m0, n0, 0, k, k, lds, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wm = wave % T::WM, wn = wave / T::WM;
-#pragma unroll
-  for (int j = 0; j < T::TN; ++j) {
-    const int n = n0 + (wn * T::TN + j) * 16 + (lane & 15);   // row of X
-#pragma unroll
-    for (int i = 0; i < T::TM; ++i) {
-      const int m = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4;   // column of X
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
-      if constexpr (LAST) {
-        if (n >= poly.rows) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (m + e >= xt.rows) continue;
-          const long at = blockIdx.z * u.o_batch + (across ? (long)(m + e) * u.o_stride + n : (long)n * u.o_stride + m + e);
-          if (u.o_bf16) static_cast<uint16_t*>(o)[at] = bf16_bits(u.scale * v[e]);
-          else static_cast<float*>(o)[at] = u.scale * v[e];
-        }
+      if (parts) {
+        if (n < s.r && m < part_ld)
+          *reinterpret_cast<f32x4*>(parts + blockIdx.y * part + ((long)blockIdx.z * s.r + n) * part_ld + m) = acc[i][j];
       } else {
-        if (n < poly.rows && m < p.x_ld)
-          put<T::NP>(p.x + blockIdx.z * p.x_batch + (long)n * p.x_ld + m, p.x_plane, v);
-        if (n < p.xt_ld)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (m + e >= xt.rows) continue;
-            uint16_t q[T::NP];
-            cut<T::NP>(v[e], q);
-#pragma unroll
-            for (int s = 0; s < T::NP; ++s)
-              p.xt[s * p.xt_plane + blockIdx.z * p.xt_batch + (long)(m + e) * p.xt_ld + n] = q[s];
-          }
+        finish<KIND>(s, m, n, acc[i][j], tm != tn);
       }
     }
   }
 }
 
-template <int NP>
-hipError_t update(const UpdateArgs& a, const void* g, void* o, char* ws, hipStream_t st) {
-  typedef Tile<128, 128, 2, 2, NP> T;
-  const UpdateLayout l = update_layout(a);
-  const int across = a.rows > a.cols;
-  double* norms = reinterpret_cast<double*>(ws + l.norms);
-  wino_launch(k_update_norm, dim3(kNormParts, a.batch), dim3(256), st, g, a, norms);
-  const long xb = (long)l.r * l.cp, tb = (long)l.c * l.rp, sb = (long)l.r * l.rp;
-  Planes p[2];
-  for (int i = 0; i < 2; ++i)
-    p[i] = Planes{reinterpret_cast<uint16_t*>(ws + (i ? l.x2 : l.x)), reinterpret_cast<uint16_t*>(ws + (i ? l.xt2 : l.xt)),
-                  l.cp, xb * a.batch, xb, l.rp, tb * a.batch, tb};
-  uint16_t* gram = reinterpret_cast<uint16_t*>(ws + l.gram);
-  uint16_t* poly = reinterpret_cast<uint16_t*>(ws + l.poly);
-  wino_launch((k_update_planes<NP>), dim3(l.cp / 64, l.rp / 64, a.batch), dim3(256), st, g, a, l.r, l.c, across,
-              (const double*)norms, p[0]);
-  const int tr = (l.rp + T::BM - 1) / T::BM, tc = (l.cp + T::BM - 1) / T::BM;
-  const Symmetric sg{gram, l.rp, sb * a.batch, sb, l.r}, sp{poly, l.rp, sb * a.batch, sb, l.r};
-  const Operand og{gram, l.rp, sb * a.batch, sb, l.r}, op{poly, l.rp, sb * a.batch, sb, l.r};
-  for (int s = 0; s < a.steps; ++s) {
-    const Planes& from = p[s & 1];
-    const Operand ox{from.x, l.cp, xb * a.batch, xb, l.r}, ot{from.xt, l.rp, tb * a.batch, tb, l.c};
-    wino_launch((k_update_symmetric<T, false>), dim3(tr * tr, 1, a.batch), dim3(T::THREADS), st, ox, sg, l.cp, tr, a.a,
-                a.b, a.c);
-    wino_launch((k_update_symmetric<T, true>), dim3(tr * tr, 1, a.batch), dim3(T::THREADS), st, og, sp, l.rp, tr, a.a,
-                a.b, a.c);
-    if (s + 1 < a.steps)
-      wino_launch((k_update_next<T, false>), dim3(tc * tr, 1, a.batch), dim3(T::THREADS), st, ot, op, p[~s & 1], l.rp,
-                  tc, a, across, o);
-    else
-      wino_launch((k_update_next<T, true>), dim3(tc * tr, 1, a.batch), dim3(T::THREADS), st, ot, op, p[~s & 1], l.rp,
-                  tc, a, across, o);
+// Sums of the ranges of a symmetric product's k, tiles of 64 x 64.
+template <Kind KIND>
+__global__ __launch_bounds__(256) void k_update_join(const float* __restrict__ parts, int count, long part,
+                                                     int part_ld, Result s) {
+  int tm, tn;
+  triangle(blockIdx.x, tm, tn);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = tn * 64 + wave * 16 + (lane & 15), m = tm * 64 + i * 16 + (lane >> 4) * 4;
+    f32x4 v = {0, 0, 0, 0};
+    if (n < s.r && m < part_ld)
+      for (int q = 0; q < count; ++q)
+        v += *reinterpret_cast<const f32x4*>(parts + q * part + ((long)blockIdx.z * s.r + n) * part_ld + m);
+    finish<KIND>(s, m, n, v, tm != tn);
   }
-  return hipGetLastError();
+}
+
+// Products of few tiles, where waiting counts: 32 x 32 of D a wave, fragments straight from memory
+// into registers, no barrier in the loop.  SHARE: the four waves of a work group take every fourth
+// block of k and join their sums in LDS; otherwise they are 2 x 2 over a tile of 64 x 64.
+template <bool SHARE, Kind KIND>
+__global__ __launch_bounds__(256) void k_update_few(Operand x, Operand y, int k, int tiles_m, Result s) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int SIDE = SHARE ? 32 : 64, DEPTH = 4;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m0 = blockIdx.x % tiles_m * SIDE + (SHARE ? 0 : (wave & 1) * 32);
+  const int n0 = blockIdx.x / tiles_m * SIDE + (SHARE ? 0 : (wave >> 1) * 32);
+  if (!SHARE && (m0 >= x.rows || n0 >= y.rows)) return;   // nothing there, not even zeros to write
+  __amdgpu_buffer_rsrc_t rx[2], ry[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    rx[q] = rows_of<true>(x, q, blockIdx.z, m0, 32, k);
+    ry[q] = rows_of<true>(y, q, blockIdx.z, n0, 32, k);
+  }
+  const int at[4] = {lane * 16, (int)x.ld * 2 + lane * 16, lane * 16, (int)y.ld * 2 + lane * 16};
+  f32x4 acc[2][2] = {};
+  const int blocks = k / 32, first = SHARE ? wave : 0, step = SHARE ? 4 : 1;
+  for (int b = first; b < blocks; b += DEPTH * step) {
+    u32x4 fx[DEPTH][2][2], fy[DEPTH][2][2];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      // beyond the last block: any block, multiplied by nothing
+      const int to = (b + d * step < blocks ? b + d * step : b) * 1024;
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          fx[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx[q], at[i], to, 0));
+          fy[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry[q], at[2 + i], to, 0));
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      if (b + d * step >= blocks) break;
+#pragma unroll
+      for (int t = 1; t >= 0; --t)
+#pragma unroll
+        for (int q = 0; q <= t; ++q)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = multiply_block<2>(fx[d][q][i], fy[d][t - q][j], acc[i][j]);
+    }
+  }
+  if constexpr (SHARE) {
+    __shared__ f32x4 join[4][4][64];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) join[wave][i * 2 + j][lane] = acc[i][j];
+    __syncthreads();
+    // one of the four 16 x 16 blocks a wave
+    f32x4 v = join[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) v += join[w][wave][lane];
+    finish<KIND>(s, m0 + (wave >> 1) * 16 + (lane >> 4) * 4, n0 + (wave & 1) * 16 + (lane & 15), v, false);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        finish<KIND>(s, m0 + i * 16 + (lane >> 4) * 4, n0 + j * 16 + (lane & 15), acc[i][j], false);
+  }
+#endif
+}
+
+typedef Tile<128, 128, 2, 4, 2, 4, true> Mid;
+
+int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
+int half_of(int tiles) { return tiles * (tiles + 1) / 2; }
+
+// Few rows: the products' tiles of 128 would leave most of the chip idle.
+bool few(const UpdateLayout& l, int batch) { return (long)l.r * l.r * batch <= 256L * 256 * 4; }
+
+template <Kind KIND>
+void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& y, int k, const Result& s,
+             float* parts, hipStream_t st) {
+  const int rows_m = KIND <= kPoly ? l.r : l.c, rows_n = l.r;
+  if (few(l, batch)) {
+    if (k >= 512) {
+      const int tm = tiles_of(rows_m, 32);
+      wino_launch((k_update_few<true, KIND>), dim3(tm * tiles_of(rows_n, 32), 1, batch), dim3(256), st, x, y, k, tm, s);
+    } else {
+      const int tm = tiles_of(rows_m, 64);
+      wino_launch((k_update_few<false, KIND>), dim3(tm * tiles_of(rows_n, 64), 1, batch), dim3(256), st, x, y, k, tm,
+                  s);
+    }
+    return;
+  }
+  const int tm = tiles_of(rows_m, 128), tn = tiles_of(rows_n, 128);
+  if constexpr (KIND == kGram) {
+    const int tiles = half_of(tm), per = (int)up((k + l.splits - 1) / l.splits, 32);
+    const long part = (long)batch * l.r * l.rp;
+    wino_launch((k_update_product<Mid, KIND>), dim3(tiles, l.splits, batch), dim3(Mid::THREADS), st, x, y, k, per, tm,
+                s, l.splits > 1 ? parts : nullptr, part, l.rp);
+    if (l.splits > 1)
+      wino_launch((k_update_join<KIND>), dim3(half_of(tiles_of(l.rp, 64)), 1, batch), dim3(256), st,
+                  (const float*)parts, l.splits, part, l.rp, s);
+  } else {
+    wino_launch((k_update_product<Mid, KIND>), dim3(KIND == kPoly ? half_of(tm) : tm * tn, 1, batch),
+                dim3(Mid::THREADS), st, x, y, k, k, tm, s, (float*)nullptr, 0L, 0);
+  }
+}
+
+// Exponent that brings magnitudes up to `most` to 2^15 or below.
+int exponent(double most) {
+  int e = 0;
+  if (!(most > 1e-30)) most = 1e-30;
+  if (!(most < 1e30)) most = 1e30;
+  std::frexp(most, &e);
+  return 15 - e;
 }
 
 }  // namespace
 
 UpdateLayout update_layout(const UpdateArgs& a) {
   UpdateLayout l{};
-  l.planes = a.o_bf16 ? 2 : 3;
   l.r = a.rows < a.cols ? a.rows : a.cols;
   l.c = a.rows < a.cols ? a.cols : a.rows;
-  l.rp = (int)up(l.r, 64);
-  l.cp = (int)up(l.c, 64);
+  l.rp = (int)up(l.r, 32);
+  l.cp = (int)up(l.c, 32);
   size_t at = 0;
   const auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
-  const size_t item = 2 * (size_t)l.planes * a.batch;
+  const size_t r16 = up(l.r, 16), c16 = up(l.c, 16), item = 2 * 2 * (size_t)a.batch;   // two planes
   l.norms = take(sizeof(double) * kNormParts * a.batch);
-  l.x = take(item * l.r * l.cp);
-  l.xt = take(item * l.c * l.rp);
-  l.x2 = take(item * l.r * l.cp);
-  l.xt2 = take(item * l.c * l.rp);
-  l.gram = take(item * l.r * l.rp);
-  l.poly = take(item * l.r * l.rp);
+  l.x = take(item * r16 * l.cp);
+  l.xt = take(item * c16 * l.rp);
+  l.x2 = take(item * r16 * l.cp);
+  l.xt2 = take(item * c16 * l.rp);
+  l.gram = take(item * r16 * l.rp);
+  l.poly = take(item * r16 * l.rp);
+  l.splits = 1;
+  if (a.batch && l.r && !few(l, a.batch)) {
+    // ranges of A's k until its tiles fill the chip, each of 256 or more
+    const long tiles = (long)half_of(tiles_of(l.r, 128)) * a.batch;
+    long s = (256 + tiles - 1) / tiles;
+    if (s > l.cp / 256) s = l.cp / 256;
+    l.splits = (int)(s < 1 ? 1 : s);
+    if (l.splits > 1) l.parts = take(4 * (size_t)l.splits * a.batch * l.r * l.rp);
+  }
   l.bytes = at ? at : 256;
   return l;
 }
 
 hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, hipStream_t st) {
-  return a.o_bf16 ? update<2>(a, g, o, ws, st) : update<3>(a, g, o, ws, st);
+  const UpdateLayout l = update_layout(a);
+  const int across = a.rows > a.cols;
+  double* norms = reinterpret_cast<double*>(ws + l.norms);
+  wino_launch(k_update_norm, dim3(kNormParts, a.batch), dim3(256), st, g, a, norms);
+  const long r16 = (long)up(l.r, 16), c16 = (long)up(l.c, 16);
+  const auto planes = [&](size_t at, long rows, int k, int e) {
+    return Planes{reinterpret_cast<uint16_t*>(ws + at), rows * k * a.batch, rows * k, k / 32, e};
+  };
+  const auto operand = [](const Planes& p, long rows) { return Operand{p.p, p.kb * 512L, p.plane, p.batch, (int)rows}; };
+  // largest singular value that X can have
+  double s = 1;
+  Planes x = planes(l.x, r16, l.cp, exponent(s)), xt = planes(l.xt, c16, l.rp, exponent(s));
+  wino_launch(k_update_planes, dim3((l.cp + 63) / 64, (l.rp + 63) / 64, a.batch), dim3(256), st, g, a, l.r, l.c, across,
+              (const double*)norms, x, xt);
+  float* parts = reinterpret_cast<float*>(ws + l.parts);
+  for (int i = 0; i < a.steps; ++i) {
+    // largest |p(t)|, p(t) = a + b t + c t^2 on [0, s^2], and largest s |p(s^2)|: at the ends or where
+    // the derivative vanishes
+    const double A = a.a, B = a.b, C = a.c, end = s * s;
+    double most_p = std::fmax(std::fabs(A), std::fabs(A + B * end + C * end * end)), most_x = 0;
+    const auto at = [&](double t) {
+      if (!(t >= 0 && t <= end)) return;
+      const double p = std::fabs(A + B * t + C * t * t);
+      most_p = std::fmax(most_p, p);
+      most_x = std::fmax(most_x, std::sqrt(t) * p);
+    };
+    at(end);
+    if (C != 0) {
+      at(-B / (2 * C));
+      const double root = std::sqrt(std::fmax(0.0, 9 * B * B - 20 * A * C));
+      at((-3 * B + root) / (10 * C));
+      at((-3 * B - root) / (10 * C));
+    } else if (B != 0) {
+      at(-A / (3 * B));
+    }
+    const Planes gram = planes(l.gram, r16, l.rp, exponent(end)), poly = planes(l.poly, r16, l.rp, exponent(most_p));
+    Result q{};
+    q.r = l.r, q.c = l.c, q.a = a.a, q.b = a.b, q.c2 = a.c, q.scale = a.scale;
+    q.across = across, q.bf16 = a.o_bf16, q.o = o, q.o_batch = a.o_batch, q.o_stride = a.o_stride;
+    q.out = gram, q.e = 2 * x.e;
+    product<kGram>(l, a.batch, operand(x, l.r), operand(x, l.r), l.cp, q, parts, st);
+    q.out = poly, q.gram = gram, q.e = 2 * gram.e;
+    product<kPoly>(l, a.batch, operand(gram, l.r), operand(gram, l.r), l.rp, q, parts, st);
+    // Room for the products' roundings, and no more: the usual coefficients keep [0, 1.26] within
+    // itself, from 1.27 on every step would enlarge it.
+    s = 1.0001 * most_x;
+    const bool odd = i & 1;
+    const Planes x2 = planes(odd ? l.x : l.x2, r16, l.cp, exponent(s)), xt2 = planes(odd ? l.xt : l.xt2, c16, l.rp, exponent(s));
+    q.out = x2, q.out_t = xt2, q.e = xt.e + poly.e;
+    if (i + 1 < a.steps) product<kNext>(l, a.batch, operand(xt, l.c), operand(poly, l.r), l.rp, q, parts, st);
+    else product<kLast>(l, a.batch, operand(xt, l.c), operand(poly, l.r), l.rp, q, parts, st);
+    x = x2, xt = xt2;
+  }
+  return hipGetLastError();
 }
 
 }  // namespace wino

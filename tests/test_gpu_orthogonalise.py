@@ -2,8 +2,8 @@
 
 Tolerance.  With f(s) = a s + b s^3 + c s^5 on the singular values, |f'| <= 4 on [0, 1.2], the range
 that the usual coefficients keep them in, so an error of the matrix before a step leaves it at most four
-times as large in the Frobenius norm.  A step adds three products of factors with errors of q each
-(2^-24 kept of fp32's, 3 x 2^-16 for results in bf16: two planes hold 16 bits) and fp32 sums that behave like random
+times as large in the Frobenius norm.  A step adds three products, q = 3 x 2^-22 each (both factors held
+to 2^-22 of themselves by two planes of fp16, and the product of their lower planes left out) and fp32 sums that behave like random
 walks of their length n, u (8 + 2 sqrt(n)), each relative to |X| times the size of the polynomial's terms, at most a + |b| +
 |c| = 10.3 for singular values up to one.  So the result's error is at most the sum over the steps of
 4^(steps - k) 10.3 (3 q + u (8 + 2 sqrt(n))) max(|X_k|, |X_(k+1)|), and half a step of a bf16 result.
@@ -37,7 +37,7 @@ def dtype_of(name):
 
 
 def compare(got, g, o_type, steps=5, scale=1.0):
-    q = U if o_type == "f32" else 3 * 2.0 ** -16
+    q = 3 * 2.0 ** -22
     for i in range(len(g)):
         ref, norms = tr.orthogonalise(g[i], steps=steps, scale=scale)
         norms = norms + [np.linalg.norm(ref) / abs(scale)]
@@ -114,7 +114,7 @@ def test_magnitudes(scale):
     desc = wn.OrthogonaliseDesc(1, 33, 70, eps=eps)
     wn.wino_orthogonalise(desc, g, o, room(wn, desc))
     ref, norms = tr.orthogonalise(g[0].double().cpu().numpy(), eps=eps)
-    step = 10.3 * (3 * U + U * (8 + 2 * np.sqrt(70)))
+    step = 10.3 * (9 * 2.0 ** -22 + U * (8 + 2 * np.sqrt(70)))
     tol = sum(4.0 ** (5 - k) * step * max(norms[k - 1], np.linalg.norm(ref)) for k in range(1, 6))
     assert np.linalg.norm(o[0].double().cpu().numpy() - ref) <= tol
 
