@@ -443,7 +443,8 @@ int wino_layer_norm_backward(const wino_norm_desc_t* d, const void* dy, const vo
  * out: loss 0, no gradient, whatever h holds there; its lse is still that of h.  Classes may
  * be masked by a bias of -infinity: a masked target's loss is +infinity; a row
  * with every class masked has lse -infinity, loss +infinity and no gradient.
- * Products of fp32 operands keep 24 bits of each factor. */
+ * Products of fp32 operands take 22 bits of each factor (of values below 2^-18
+ * of the tensor's largest: 2^-39 of that) and sum in fp32. */
 enum { WINO_LOSS_MAX_ROWS = 1 << 21, WINO_LOSS_MAX_FEATURES = 1 << 20, WINO_LOSS_MAX_CLASSES = 1 << 27 };
 typedef struct {
   int rows, features, classes;
@@ -462,8 +463,9 @@ int wino_linear_cross_entropy(const wino_loss_desc_t* d, const void* h, const vo
  *   dl_tv = (exp(l_tv - lse_t) - [v = target_t]) dloss_t,
  *   dh = dl w,  dw = dl^T h,  dbias = sum_t dl
  * dh [rows][features] and dw [classes][features] dense, of `type`; dbias
- * [classes] fp32; each may be null.  bf16: dl / max|dloss| is rounded to bf16
- * before the two products (dbias sums it unrounded).  Without rows dw and dbias
+ * [classes] fp32; each may be null.  Before the two products dl / max|dloss| is
+ * rounded, for bf16 to bf16, for fp32 like the other factors (dbias sums it
+ * unrounded).  Without rows dw and dbias
  * are zeros. */
 int wino_linear_cross_entropy_backward_workspace_bytes(const wino_loss_desc_t* d, size_t* bytes);
 int wino_linear_cross_entropy_backward(const wino_loss_desc_t* d, const void* h, const void* w,

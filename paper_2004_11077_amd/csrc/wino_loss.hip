@@ -5,14 +5,17 @@
 //
 // Forward: the logits of a tile leave the matrix instructions in registers and end there as a maximum
 // and a sum of exponentials a row; those of all tiles are joined by a second kernel.  Backward: the
-// logits are computed again, piece by piece of the classes, and become dl in the workspace, once as
-// rows and once as columns, which are the operands of the two products of the piece.
+// logits are computed again, piece by piece of the classes, and become dl in the workspace, the
+// operand of the two products of the piece; h, W and dl enter those with k across their rows
+// (wino_products.hpp), so none of them is transposed in memory.
 //
-// dl is kept on as many bf16 planes as the operands have (wino_products.hpp): one for bf16 operands,
-// a rounding of half a step like the one that h, W and the gradients have; three, nothing lost, for
-// fp32.  It is kept relative to the largest |dloss|, by which the products' results are multiplied in
-// fp32: with one weight for all rows, as for a mean, the -1 of a target's class stays free of a
-// rounding that would be the same in every row.
+// bf16 operands are taken where they lie if their rows are whole blocks of 16 bytes and of 32 k, and
+// from a padded copy otherwise; dl is rounded to bf16 like the gradients.  fp32 operands become two
+// fp16 planes (22 bits) under one power of two for W and one for h (in the forward pass one a row, so that
+// no row's magnitude touches another's lse); in the backward pass rows that are left out count as
+// zeros, whatever they hold, and do not enter the power of two.  dl is kept relative to the largest
+// |dloss|, by which the products' results are multiplied in fp32: with one weight for all rows, as
+// for a mean, the -1 of a target's class stays free of a rounding that would be the same in every row.
 #include "wino_products.hpp"
 #include "wino_train.hpp"
 
@@ -21,105 +24,217 @@ namespace {
 
 using namespace prod;
 
-// exp(x) for x <= 0 or so: exp2 of x log2(e), the part of the product that fp32 loses added back.
-__device__ __forceinline__ float exp_of(float x) {
-  x = x < -150.f ? -150.f : x;   // a NaN stays one; exp(-150) is 0 in fp32
-  const float t = x * 1.44269504f;
-  const float r = __builtin_fmaf(x, 1.44269504f, -t) + x * 1.925963033e-8f;
-  return __builtin_amdgcn_exp2f(t) * __builtin_fmaf(r, 0.69314718f, 1.f);
+constexpr int kRange = 256;        // partial maxima of a tensor
+constexpr int kDlExponent = 15;    // fp16 planes of dl: |dl| <= 1 relative to the largest |dloss|
+constexpr float kInf = __builtin_inff();
+
+// Numbers that kernels hand to later ones.
+struct Numbers {
+  float ref;              // largest |dloss|
+  float of_w, of_h;       // what a value in W's, h's planes has to be multiplied by
+  float pad;
+  float max_w[kRange], max_h[kRange];
+};
+
+// exp(x) for x <= 0 or so by exp2; the argument's rounding is |x| 2^-24, which is most where exp is
+// least.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// 2^e with |x| 2^e <= 2^15 for |x| <= most.
+__device__ __forceinline__ int exponent_for(float most) {
+  const int e = 15 - __builtin_amdgcn_frexp_expf(most);
+  return most == 0.f ? 0 : e > 120 ? 120 : e;
 }
 
-// src [rows][cols] (fp32 or bf16) -> planes [rows][ld], columns from cols to ld zero.
+// Maximum over the 256 threads of a work group.
+__device__ __forceinline__ float group_max(float m, float* lds) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = lds[0];
+  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) m = __builtin_fmaxf(m, lds[w]);
+  return m;
+}
+
+// What tells the rows that count.
+struct Rows {
+  const int64_t* target;
+  long ignore;
+  int rows, classes;
+  __device__ __forceinline__ bool kept(int t) const {
+    const long c = target[t];
+    return c != ignore && c >= 0 && c < classes;
+  }
+};
+
+// Largest finite |x| of the rows of a tensor that blockIdx.x has.
+__device__ __forceinline__ float range_of(const float* x, long ld, int rows, int cols, const Rows* g, float* lds) {
+  float m = 0;
+  const auto take = [&](float v) {
+    v = __builtin_fabsf(v);
+    m = v < kInf ? __builtin_fmaxf(m, v) : m;
+  };
+  if (!g && ld == cols) {   // one run of values
+    const long items = (long)rows * cols;
+#pragma unroll 8
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += kRange * 256) take(x[i]);
+  } else {
+    for (int r = blockIdx.x; r < rows; r += kRange) {
+      if (g && !g->kept(r)) continue;
+      for (int c = threadIdx.x; c < cols; c += 256) take(x[(long)r * ld + c]);
+    }
+  }
+  return group_max(m, lds);
+}
+
+// First kernel of a call: the largest |dloss| of the rows that count, and for fp32 the ranges of W and
+// of h's rows that count.
+__global__ __launch_bounds__(256) void k_loss_range(const float* __restrict__ w, long w_ld,
+                                                    const float* __restrict__ h, long h_ld, int features, Rows g,
+                                                    const float* __restrict__ dloss, Numbers* __restrict__ to) {
+  __shared__ float lds[4];
+  if (dloss && blockIdx.x == 0) {
+    float m = 0;
+    for (int t = threadIdx.x; t < g.rows; t += 256)
+      if (g.kept(t)) m = __builtin_fmaxf(m, __builtin_fabsf(dloss[t]));
+    m = group_max(m, lds);
+    if (threadIdx.x == 0) to->ref = m;
+  }
+  if (w) {
+    const float m = range_of(w, w_ld, g.classes, features, nullptr, lds);
+    if (threadIdx.x == 0) to->max_w[blockIdx.x] = m;
+  }
+  if (h) {
+    const float m = range_of(h, h_ld, g.rows, features, &g, lds);
+    if (threadIdx.x == 0) to->max_h[blockIdx.x] = m;
+  }
+}
+
+// One tensor to planes: [rows][cols] -> [rows][ld], columns from cols to ld zero.
+struct Copy {
+  const void* src;
+  long src_ld;
+  int rows, cols;
+  uint16_t* dst;
+  int ld;
+  long plane;
+  int masked;             // rows that do not count as zeros
+  const float* most;      // fp32: [kRange] partial maxima, null: one power of two a row, to `unit`
+  float* unit;
+};
+
 template <class T, int NP>
-__global__ __launch_bounds__(256) void k_planes(const T* __restrict__ src, long src_ld, int rows, int cols,
-                                                uint16_t* __restrict__ dst, long ld, long plane) {
-  const long each = ld / 8;
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < rows * each; i += (long)gridDim.x * 256) {
-    const long r = i / each;
+__device__ __forceinline__ void copy_rows(const Copy& o, const Rows& g, unsigned block, unsigned blocks, float* lds) {
+  float scale = 1;
+  if constexpr (NP == 2) {
+    const int e = exponent_for(group_max(o.most[threadIdx.x], lds));
+    scale = power(e);
+    if (block == 0 && threadIdx.x == 0) *o.unit = power(-e);
+  }
+  const unsigned each = o.ld / 8;
+  const long items = (long)o.rows * each;
+  for (long i = (long)block * 256 + threadIdx.x; i < items; i += (long)blocks * 256) {
+    const long r = i >> 32 ? i / each : (long)((unsigned)i / each);
     const int c = (int)(i - r * each) * 8;
+    const bool in = !o.masked || g.kept((int)r);
     __attribute__((aligned(16))) uint16_t out[NP][8];
+    const T* p = static_cast<const T*>(o.src) + r * o.src_ld + c;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       uint16_t q[NP] = {};
-      if (c + e < cols) {
-        if constexpr (sizeof(T) == 2) q[0] = src[r * src_ld + c + e];
-        else cut<NP>(src[r * src_ld + c + e], q);
+      if (in && c + e < o.cols) {
+        if constexpr (NP == 1) q[0] = p[e];
+        else cut<2>(p[e] * scale, q);
       }
 #pragma unroll
-      for (int p = 0; p < NP; ++p) out[p][e] = q[p];
+      for (int n = 0; n < NP; ++n) out[n][e] = q[n];
     }
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
-      *reinterpret_cast<uint4*>(dst + p * plane + r * ld + c) = *reinterpret_cast<const uint4*>(out[p]);
+    for (int n = 0; n < NP; ++n)
+      *reinterpret_cast<uint4*>(o.dst + n * o.plane + r * o.ld + c) = *reinterpret_cast<const uint4*>(out[n]);
   }
 }
 
-// src [rows][cols] -> planes [cols][ld], dst[c][r] = src[r][c]; zero for r from rows to ld.  With
-// `target`, rows whose target is no class count as zeros whatever they hold.
+// fp32 rows, each under a power of two of its own: one wave a row.
+__device__ __forceinline__ void copy_rows_apart(const Copy& o, unsigned block, unsigned blocks) {
+  const int lane = threadIdx.x & 63;
+  for (long r = (long)block * 4 + (threadIdx.x >> 6); r < o.rows; r += (long)blocks * 4) {
+    const float* p = static_cast<const float*>(o.src) + r * o.src_ld;
+    float m = 0;
+    for (int c = lane; c < o.cols; c += 64) {
+      const float v = __builtin_fabsf(p[c]);
+      m = v < kInf ? __builtin_fmaxf(m, v) : m;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
+    const int e = exponent_for(m);
+    const float scale = power(e);
+    if (lane == 0) o.unit[r] = power(-e);
+    for (int c = lane * 2; c < o.ld; c += 128) {
+      uint16_t a[2], b[2];
+      cut<2>(c < o.cols ? p[c] * scale : 0.f, a);
+      cut<2>(c + 1 < o.cols ? p[c + 1] * scale : 0.f, b);
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        *reinterpret_cast<ushort2*>(o.dst + n * o.plane + r * o.ld + c) = make_ushort2(a[n], b[n]);
+    }
+  }
+}
+
+// W's piece and h to planes in one launch: the first `first` work groups take W.
 template <class T, int NP>
-__global__ __launch_bounds__(256) void k_planes_across(const T* __restrict__ src, long src_ld, int rows,
-                                                       int cols, uint16_t* __restrict__ dst, long ld,
-                                                       long plane, const int64_t* __restrict__ target,
-                                                       long ignore, int classes) {
-  __shared__ T tile[64][64 + 4 / sizeof(T)];
-  const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int r = r0 + y + i * 4, c = c0 + x;
-    bool in = r < rows && c < cols;
-    if (target && in) {
-      const long t = target[r];
-      in = t != ignore && t >= 0 && t < classes;
-    }
-    tile[y + i * 4][x] = in ? src[(long)r * src_ld + c] : (T)0;
-  }
-  __syncthreads();
-  const int c = threadIdx.x >> 2, rq = (threadIdx.x & 3) * 16;
-  if (c0 + c >= cols) return;
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int r = rq + half * 8;
-    if (r0 + r >= ld) return;
-    __attribute__((aligned(16))) uint16_t out[NP][8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint16_t q[NP] = {};
-      if constexpr (sizeof(T) == 2) q[0] = tile[r + e][c];
-      else cut<NP>(tile[r + e][c], q);
-#pragma unroll
-      for (int p = 0; p < NP; ++p) out[p][e] = q[p];
-    }
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-      *reinterpret_cast<uint4*>(dst + p * plane + (long)(c0 + c) * ld + r0 + r) =
-          *reinterpret_cast<const uint4*>(out[p]);
-  }
+__global__ __launch_bounds__(256) void k_loss_planes(Copy w, Copy h, unsigned first, Rows g) {
+  __shared__ float lds[4];
+  if (blockIdx.x < first) copy_rows<T, NP>(w, g, blockIdx.x, first, lds);
+  else if (NP == 2 && !h.most) copy_rows_apart(h, blockIdx.x - first, gridDim.x - first);
+  else copy_rows<T, NP>(h, g, blockIdx.x - first, gridDim.x - first, lds);
 }
 
 // What the logits of a piece need besides the operands.
 struct Logits {
-  const float* bias;        // of all classes, may be null
-  const int64_t* target;
-  long ignore;
-  int rows, classes;        // all of them
-  int first;                // first class of this piece
-  int count;                // classes of this piece
-  int k;                    // features rounded up
+  const float* bias;         // of all classes, may be null
+  Rows g;
+  int first, count;          // classes of this piece
+  int k;                     // features in whole blocks
+  const float* of_w;         // fp32: the planes' units; of h one for all rows or one a row
+  const float* of_h;
+  int h_apart;
 };
 
-// Work group of the grid -> tile (m of W's rows, n of h's rows).  Consecutive work groups go round
-// robin over the 8 XCDs: each XCD takes a run of tiles, in which bands of eight tiles of classes keep
-// their rows of W in its L2 while the rows of h pass.
-__device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& m, int& n) {
-  const int all = tiles_m * tiles_n;
-  int b = blockIdx.x;
-  const int per = all / 8;
+// Work group of the grid -> tile (m, n).  Consecutive work groups go round robin over the 8 XCDs: each
+// XCD takes a run of tiles, in which bands of eight tiles m keep their rows in its L2 while those of n
+// pass.
+__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& m, int& n) {
+  const int all = tiles_m * tiles_n, per = all / 8;
   if (b < per * 8) b = (b & 7) * per + (b >> 3);
   const int band = b / (8 * tiles_n), rest = b - band * 8 * tiles_n;
   const int wide = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
   m = band * 8 + rest % wide;
   n = rest / wide;
+}
+
+// Products -> logits of a tile: units, bias, and -infinity beyond the last class.
+template <class T>
+__device__ __forceinline__ void to_logits(const Logits& g, int v0, int j_t, f32x4 (&acc)[T::TM][T::TN], int j) {
+  if constexpr (T::NP == 2) {
+    const float u = *g.of_w * g.of_h[g.h_apart ? j_t : 0];
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] *= u;
+  }
+  if (g.bias || v0 + T::TM * 16 > g.count) {
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int v = v0 + i * 16 + e;
+        if (v >= g.count) acc[i][j][e] = -kInf;
+        else if (g.bias) acc[i][j][e] += g.bias[g.first + v];
+      }
+  }
 }
 
 // Forward: best[part][t], part = tile of classes: maximum and sum of exp(l - maximum); the target's
@@ -130,38 +245,37 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_logits(Operand w, Operand h
                                                             float* __restrict__ hit) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
-  tile_of(tiles_m, tiles_n, tm, tn);
+  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
-  multiply<T>(w, h, 0, m0, n0, 0, g.k, g.k, lds, acc);
+  multiply<T>(w, h, 0, m0, n0, 0, g.k, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
   __syncthreads();
   float2* join = reinterpret_cast<float2*>(lds);   // [WM][BN]
+  const int v0 = m0 + wm * T::TM * 16 + (lane >> 4) * 4;
 #pragma unroll
   for (int j = 0; j < T::TN; ++j) {
     const int t = n0 + (wn * T::TN + j) * 16 + (lane & 15);
-    const long cls = t < g.rows ? g.target[t] : -1;
-    const bool kept = t < g.rows && cls != g.ignore && cls >= 0 && cls < g.classes;
-    float top = -__builtin_inff();
+    const int row = t < g.g.rows ? t : g.g.rows - 1;
+    to_logits<T>(g, v0, row, acc, j);
+    // the target, counted from this lane's first class
+    const long off = t < g.g.rows && g.g.kept(t) ? g.g.target[t] - g.first - v0 : -1;
+    if (__any(off >= 0 && off < T::TM * 16)) {
+#pragma unroll
+      for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (off == i * 16 + e) hit[t] = acc[i][j][e];
+    }
+    float top = -kInf;
 #pragma unroll
     for (int i = 0; i < T::TM; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int v = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4 + e;
-        float l = acc[i][j][e];
-        if (v < g.count) {
-          if (g.bias) l += g.bias[g.first + v];
-          if (kept && cls == g.first + v) hit[t] = l;
-        } else {
-          l = -__builtin_inff();
-        }
-        acc[i][j][e] = l;
-        top = __builtin_fmaxf(top, l);
-      }
+      for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, acc[i][j][e]);
 #pragma unroll
     for (int d = 16; d < 64; d *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, d, 64));
-    const float base = top == -__builtin_inff() ? 0.f : top;
+    const float base = top == -kInf ? 0.f : top;
     float sum = 0;
 #pragma unroll
     for (int i = 0; i < T::TM; ++i)
@@ -176,117 +290,103 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_logits(Operand w, Operand h
     float top = join[i].x, sum = 0;
 #pragma unroll
     for (int q = 1; q < T::WM; ++q) top = __builtin_fmaxf(top, join[q * T::BN + i].x);
-    const float base = top == -__builtin_inff() ? 0.f : top;
+    const float base = top == -kInf ? 0.f : top;
 #pragma unroll
-    for (int q = 0; q < T::WM; ++q)
-      sum += join[q * T::BN + i].y * exp_of(join[q * T::BN + i].x - base);
-    if (n0 + i < g.rows) best[(long)(part0 + tm) * g.rows + n0 + i] = make_float2(top, sum);
+    for (int q = 0; q < T::WM; ++q) sum += join[q * T::BN + i].y * exp_of(join[q * T::BN + i].x - base);
+    if (n0 + i < g.g.rows) best[(long)(part0 + tm) * g.g.rows + n0 + i] = make_float2(top, sum);
   }
 }
 
-// The parts of a row -> loss and lse.  16 rows a work group, 16 threads each.
+// The parts of a row -> loss and lse.  256 / EACH rows a work group, EACH threads a row.
+template <int EACH>
 __global__ __launch_bounds__(256) void k_loss_join(const float2* __restrict__ best, int parts,
-                                                   const float* __restrict__ hit, Logits g,
-                                                   float* __restrict__ loss, float* __restrict__ lse) {
-  __shared__ float2 lds[16][16];
-  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
-  const int t = blockIdx.x * 16 + x;
-  float top = -__builtin_inff(), sum = 0;
+                                                   const float* __restrict__ hit, Rows g, float* __restrict__ loss,
+                                                   float* __restrict__ lse) {
+  constexpr int ROWS = 256 / EACH;
+  __shared__ float lds[2][EACH][ROWS];
+  const int x = threadIdx.x % ROWS, y = threadIdx.x / ROWS;
+  const int t = blockIdx.x * ROWS + x;
+  float top = -kInf, sum = 0;
   if (t < g.rows)
-    for (int p = y; p < parts; p += 16) {
-      const float2 b = best[(long)p * g.rows + t];
-      const float up = __builtin_fmaxf(top, b.x), base = up == -__builtin_inff() ? 0.f : up;
-      sum = sum * exp_of(top - base) + b.y * exp_of(b.x - base);
-      top = up;
-    }
-  lds[y][x] = make_float2(top, sum);
+    for (int p = y; p < parts; p += EACH) top = __builtin_fmaxf(top, best[(long)p * g.rows + t].x);
+  lds[0][y][x] = top;
   __syncthreads();
+  for (int d = EACH / 2; d > 0; d /= 2) {
+    if (y < d) lds[0][y][x] = __builtin_fmaxf(lds[0][y][x], lds[0][y + d][x]);
+    __syncthreads();
+  }
+  top = lds[0][0][x];
+  const float base = top == -kInf ? 0.f : top;
+  if (t < g.rows)
+    for (int p = y; p < parts; p += EACH) {
+      const float2 b = best[(long)p * g.rows + t];
+      sum += b.y * exp_of(b.x - base);
+    }
+  lds[1][y][x] = sum;
+  __syncthreads();
+  for (int d = EACH / 2; d > 0; d /= 2) {
+    if (y < d) lds[1][y][x] += lds[1][y + d][x];
+    __syncthreads();
+  }
   if (y != 0 || t >= g.rows) return;
-  for (int q = 1; q < 16; ++q) top = __builtin_fmaxf(top, lds[q][x].x);
-  const float base = top == -__builtin_inff() ? 0.f : top;
-  sum = 0;
-  for (int q = 0; q < 16; ++q) sum += lds[q][x].y * exp_of(lds[q][x].x - base);
-  const float all = base + __builtin_logf(sum);   // log 0 = -inf: every class masked
+  const float all = base + __builtin_logf(lds[1][0][x]);   // log 0 = -inf: every class masked
   lse[t] = all;
-  const long cls = g.target[t];
-  const bool kept = cls != g.ignore && cls >= 0 && cls < g.classes;
   float v = 0;
-  if (kept) v = hit[t] == -__builtin_inff() && !(all != all) ? __builtin_inff() : all - hit[t];
+  if (g.kept(t)) v = hit[t] == -kInf && !(all != all) ? kInf : all - hit[t];
   loss[t] = v;
 }
 
-// The largest |dloss| of the rows that count.
-__global__ __launch_bounds__(1024) void k_loss_weight(const float* __restrict__ dloss, Logits g,
-                                                      float* __restrict__ ref) {
-  __shared__ float lds[16];
-  float m = 0;
-  for (int t = threadIdx.x; t < g.rows; t += 1024) {
-    const long cls = g.target[t];
-    if (cls != g.ignore && cls >= 0 && cls < g.classes) m = __builtin_fmaxf(m, __builtin_fabsf(dloss[t]));
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 16; ++w) m = __builtin_fmaxf(m, lds[w]);
-    *ref = m;
-  }
-}
-
-// Backward: dl / ref of a piece, as rows dl [t][piece] and as columns dlt [v][tp]; the sums over a
-// tile's rows for dbias.
+// Backward: dl / ref of a piece, rows [t][ld]; the sums over a wave's rows for dbias.
 template <class T>
 __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand h, Logits g, int tiles_m,
                                                              int tiles_n, const float* __restrict__ lse,
                                                              const float* __restrict__ dloss,
                                                              const float* __restrict__ ref,
-                                                             uint16_t* __restrict__ dl, long dl_ld, long dl_plane,
-                                                             uint16_t* __restrict__ dlt, long dlt_ld,
-                                                             long dlt_plane, float* __restrict__ dbias) {
+                                                             uint16_t* __restrict__ dl, int ld, long plane,
+                                                             float* __restrict__ dbias) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
-  tile_of(tiles_m, tiles_n, tm, tn);
+  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
-  multiply<T>(w, h, 0, m0, n0, 0, g.k, g.k, lds, acc);
+  multiply<T>(w, h, 0, m0, n0, 0, g.k, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
   const float scale = *ref;
-  float sums[T::TM][4] = {};
+  const int v0 = m0 + wm * T::TM * 16 + (lane >> 4) * 4;
 #pragma unroll
   for (int j = 0; j < T::TN; ++j) {
     const int t = n0 + (wn * T::TN + j) * 16 + (lane & 15);
-    const long cls = t < g.rows ? g.target[t] : -1;
-    const bool kept = t < g.rows && cls != g.ignore && cls >= 0 && cls < g.classes;
-    const float all = kept ? lse[t] : 0.f;
-    float weight = kept && all != -__builtin_inff() ? dloss[t] / scale : 0.f;
-    if (scale == 0.f) weight = 0.f;
+    const int row = t < g.g.rows ? t : g.g.rows - 1;
+    to_logits<T>(g, v0, row, acc, j);
+    const bool kept = t < g.g.rows && g.g.kept(row);
+    const float all = kept ? lse[row] : 0.f;
+    float weight = kept && all != -kInf && scale != 0.f ? dloss[row] / scale : 0.f;
+    const long off = kept ? g.g.target[row] - g.first - v0 : -1;
+    const bool near = __any(off >= 0 && off < T::TM * 16);
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
-      const int v = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4;
+      f32x4 d = acc[i][j];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d[e] = exp_of(d[e] - all);
+      if (near)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[e] -= off == i * 16 + e ? 1.f : 0.f;
       uint16_t out[4][T::NP];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float d = 0;
-        if (v + e < g.count && weight != 0.f) {
-          float l = acc[i][j][e];
-          if (g.bias) l += g.bias[g.first + v + e];
-          d = (exp_of(l - all) - (cls == g.first + v + e ? 1.f : 0.f)) * weight;
-        }
-        sums[i][e] += d;
-        cut<T::NP>(d, out[e]);
+        // a row that is left out gives zeros, whatever its logits are
+        d[e] = weight == 0.f ? 0.f : d[e] * weight;
+        if constexpr (T::NP == 2) cut<2>(d[e] * (float)(1 << kDlExponent), out[e]);
+        else cut<1>(d[e], out[e]);
       }
+      acc[i][j] = d;
+      const int v = v0 + i * 16;
+      if (t < g.g.rows && v < ld) {   // ld is a multiple of 4; from the last class on d is zero
 #pragma unroll
-      for (int p = 0; p < T::NP; ++p) {
-        if (t < g.rows && v < dl_ld) {   // dl_ld is a multiple of 4
-          ushort4 q = make_ushort4(out[0][p], out[1][p], out[2][p], out[3][p]);
-          *reinterpret_cast<ushort4*>(dl + p * dl_plane + (long)t * dl_ld + v) = q;
-        }
-        if (t < dlt_ld)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (v + e < g.count) dlt[p * dlt_plane + (long)(v + e) * dlt_ld + t] = out[e][p];
+        for (int p = 0; p < T::NP; ++p)
+          *reinterpret_cast<ushort4*>(dl + p * plane + (long)t * ld + v) =
+              make_ushort4(out[0][p], out[1][p], out[2][p], out[3][p]);
       }
     }
   }
@@ -295,76 +395,101 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
   for (int i = 0; i < T::TM; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float s = sums[i][e];
+      float s = acc[i][0][e];
+#pragma unroll
+      for (int j = 1; j < T::TN; ++j) s += acc[i][j][e];
 #pragma unroll
       for (int d = 1; d < 16; d *= 2) s += __shfl_xor(s, d, 64);
-      const int v = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4 + e;
-      if ((lane & 15) == 0 && v < g.count) dbias[(long)(tn * T::WN + wn) * g.classes + g.first + v] = s;
+      const int v = v0 + i * 16 + e;
+      if ((lane & 15) == 0 && v < g.count) dbias[(long)(tn * T::WN + wn) * g.g.classes + g.first + v] = s;
     }
 }
 
-__global__ __launch_bounds__(256) void k_loss_dbias(const float* __restrict__ parts, int count, int classes,
-                                                    const float* __restrict__ ref, float* __restrict__ dbias) {
-  const int v = blockIdx.x * 256 + threadIdx.x;
-  if (v >= classes) return;
-  float s = 0;
-#pragma unroll 4
-  for (int p = 0; p < count; ++p) s += parts[(long)p * classes + v];
-  dbias[v] = s * *ref;
-}
-
-// out[n][m] = ref (sum_k A[m][k] B[n][k]): the gradient of a row n of W resp. h over its features m.
+// out[n][m] = sum_k A(m, k) B(n, k): the gradient of row n of W resp. h over its features m.
 // kind 0: to fp32, 1: to bf16, both times ref; 2: to fp32 sums of a range of k (blockIdx.y), kept as
 // they are, 3: added to what is there.
 struct Product {
   void* out;
   long ld, split;        // elements between rows and between ranges of k
   int kind, k, per;      // k in all and per range
-  const float* ref;
+  int m, n;              // features and rows
+  const float *ref, *unit;
 };
 template <class T>
 __global__ __launch_bounds__(T::THREADS) void k_loss_product(Operand a, Operand b, Product p, int tiles_m,
                                                              int tiles_n) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
-  tile_of(tiles_m, tiles_n, tm, tn);
+  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
   const int k0 = blockIdx.y * p.per, k1 = k0 + p.per < p.k ? k0 + p.per : p.k;
-  multiply<T>(a, b, 0, m0, n0, k0, k1, p.k, lds, acc);
+  multiply<T>(a, b, 0, m0, n0, k0, k1, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
-  const float scale = p.kind < 2 ? *p.ref : 1.f;
+  float scale = p.kind < 2 ? *p.ref : 1.f;
+  float unit = 1.f;
+  if constexpr (T::NP == 2) unit = *p.unit * (1.f / (1 << kDlExponent));
+  const bool whole = (p.ld & 3) == 0;   // rows of out start on four elements
 #pragma unroll
   for (int j = 0; j < T::TN; ++j) {
     const int n = n0 + (wn * T::TN + j) * 16 + (lane & 15);
-    if (n >= b.rows) continue;
+    if (n >= p.n) continue;
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
       const int m = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4;
+      if (m >= p.m) continue;
       const long at = blockIdx.y * p.split + (long)n * p.ld + m;
+      f32x4 v = acc[i][j];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (m + e >= a.rows) continue;
-        const float v = acc[i][j][e] * scale;
-        if (p.kind == 1) static_cast<uint16_t*>(p.out)[at + e] = bf16_bits(v);
-        else if (p.kind == 3) static_cast<float*>(p.out)[at + e] += v;
-        else static_cast<float*>(p.out)[at + e] = v;
+      for (int e = 0; e < 4; ++e) v[e] = v[e] * unit * scale;
+      if (p.kind == 1) {
+        uint16_t* o = static_cast<uint16_t*>(p.out) + at;
+        if (whole && ((uintptr_t)p.out & 7) == 0) {
+          *reinterpret_cast<ushort4*>(o) = make_ushort4(bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m + e < p.m) o[e] = bf16_bits(v[e]);
+        }
+      } else {
+        float* o = static_cast<float*>(p.out) + at;
+        if (whole && ((uintptr_t)p.out & 15) == 0) {
+          if (p.kind == 3) v += *reinterpret_cast<const f32x4*>(o);
+          *reinterpret_cast<f32x4*>(o) = v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m + e < p.m) o[e] = p.kind == 3 ? o[e] + v[e] : v[e];
+        }
       }
     }
   }
 }
 
-// Sums of the ranges of k -> gradient.
-__global__ __launch_bounds__(256) void k_loss_sums(const float* __restrict__ sums, int count, long split,
-                                                   long items, int bf16, const float* __restrict__ ref,
-                                                   void* __restrict__ out) {
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long)gridDim.x * 256) {
-    float s = 0;
-    for (int q = 0; q < count; ++q) s += sums[q * split + i];
-    s *= *ref;
-    if (bf16) static_cast<uint16_t*>(out)[i] = bf16_bits(s);
-    else static_cast<float*>(out)[i] = s;
+// Last kernel of the backward pass: sums of the ranges of k -> dh (the first `first` work groups), and
+// of the waves' rows -> dbias.
+__global__ __launch_bounds__(256) void k_loss_sums(const float* __restrict__ sums, int count, long items, int bf16,
+                                                   void* __restrict__ out, unsigned first,
+                                                   const float* __restrict__ parts, int part_count, int classes,
+                                                   float* __restrict__ dbias, const float* __restrict__ ref) {
+  const float scale = *ref;
+  if (blockIdx.x < first) {
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long)first * 256) {
+      float s = 0;
+      for (int q = 0; q < count; ++q) s += sums[q * items + i];
+      s *= scale;
+      if (bf16) static_cast<uint16_t*>(out)[i] = bf16_bits(s);
+      else static_cast<float*>(out)[i] = s;
+    }
+  } else {
+    const long step = (long)(gridDim.x - first) * 256;
+    for (long v = (long)(blockIdx.x - first) * 256 + threadIdx.x; v < classes; v += step) {
+      float s = 0;
+#pragma unroll 4
+      for (int p = 0; p < part_count; ++p) s += parts[(long)p * classes + v];
+      dbias[v] = s * scale;
+    }
   }
 }
 
@@ -372,80 +497,100 @@ __global__ __launch_bounds__(256) void k_loss_zero(uint16_t* p, long items) {
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long)gridDim.x * 256) p[i] = 0;
 }
 
-unsigned grid_of(long items) {
+unsigned grid_of(long items, long most) {
   const long b = (items + 255) / 256;
-  return (unsigned)(b < 1 ? 1 : b < 16384 ? b : 16384);
+  return (unsigned)(b < 1 ? 1 : b < most ? b : most);
 }
 
-template <int NP>
-using TileFor = Tile<128, 128, 2, 2, NP, NP == 1 ? 4 : 3>;
-constexpr int kBM = 128, kBN = 128, kWN = 2;
+// Tiles.  256 x 256 where they fill the chip, else 128 x 128, else 64 x 64.
+template <int NP, bool AX, bool BX>
+struct Tiles {
+  typedef Tile<256, 256, 2, 4, NP, NP == 1 ? 4 : 2, AX, BX> Big;
+  typedef Tile<128, 128, 2, NP == 1 ? 2 : 4, NP, 4, AX, BX> Mid;
+  typedef Tile<64, 64, 2, 2, NP, 4, AX, BX> Small;
+};
+long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
+int side_for(long m, long n, long splits = 1) {
+  return count_of(m, n, 256) * splits >= 160 ? 256 : count_of(m, n, 128) * splits >= 160 ? 128 : 64;
+}
+constexpr int waves_n(int side, int np) { return side == 256 ? 4 : side == 128 && np == 2 ? 4 : 2; }
 
-// bf16 rows that the products can take where they lie: whole stages of features, 16-byte accesses.
+template <int NP, bool AX, bool BX, class F>
+void with_tile(int side, F&& f) {
+  if (side == 256) f(typename Tiles<NP, AX, BX>::Big{});
+  else if (side == 128) f(typename Tiles<NP, AX, BX>::Mid{});
+  else f(typename Tiles<NP, AX, BX>::Small{});
+}
+
+// bf16 rows that the products can take where they lie: 16-byte accesses, whole blocks of k.
 bool direct(const LossArgs& a, const void* p, long stride) {
-  return a.bf16 && a.features % 64 == 0 && stride % 8 == 0 && stride <= kMaxLd && ((uintptr_t)p & 15) == 0;
-}
-
-template <int NP>
-Operand planes_of(const LossArgs& a, const void* src, long src_ld, int rows, char* to, int ld, hipStream_t st) {
-  const long plane = (long)rows * ld;
-  uint16_t* dst = reinterpret_cast<uint16_t*>(to);
-  if (a.bf16)
-    wino_launch((k_planes<uint16_t, NP>), dim3(grid_of(plane / 8)), dim3(256), st, (const uint16_t*)src, src_ld, rows,
-                a.features, dst, (long)ld, plane);
-  else
-    wino_launch((k_planes<float, NP>), dim3(grid_of(plane / 8)), dim3(256), st, (const float*)src, src_ld, rows,
-                a.features, dst, (long)ld, plane);
-  return Operand{dst, ld, plane, 0, rows};
-}
-
-template <int NP>
-Operand across(const LossArgs& a, const void* src, long src_ld, int rows, char* to, int ld,
-               const int64_t* target, hipStream_t st) {
-  const long plane = (long)a.features * ld;
-  uint16_t* dst = reinterpret_cast<uint16_t*>(to);
-  const dim3 grid((rows + 63) / 64, (a.features + 63) / 64);
-  if (a.bf16)
-    wino_launch((k_planes_across<uint16_t, NP>), grid, dim3(256), st, (const uint16_t*)src, src_ld, rows, a.features,
-                dst, (long)ld, plane, target, a.ignore_index, a.classes);
-  else
-    wino_launch((k_planes_across<float, NP>), grid, dim3(256), st, (const float*)src, src_ld, rows, a.features, dst,
-                (long)ld, plane, target, a.ignore_index, a.classes);
-  return Operand{dst, ld, plane, 0, a.features};
+  return a.bf16 && a.features % 32 == 0 && stride % 8 == 0 && stride <= kMaxLd && ((uintptr_t)p & 15) == 0;
 }
 
 const void* row_at(const LossArgs& a, const void* p, long row, long stride) {
   return static_cast<const char*>(p) + row * stride * (a.bf16 ? 2 : 4);
 }
 
+// Operands of a piece: where they lie, or planes made here.
+template <int NP>
+void operands(const LossArgs& a, const LossLayout& l, const Rows& g, const void* w_rows, int count, const void* h,
+              bool w_direct, bool h_ready, bool h_apart, bool masked, Numbers* num, char* ws, Operand* ow, Operand* oh,
+              hipStream_t st) {
+  uint16_t* to_w = reinterpret_cast<uint16_t*>(ws + l.w);
+  uint16_t* to_h = reinterpret_cast<uint16_t*>(ws + l.h);
+  const long pw = (long)count * l.dp, ph = (long)a.rows * l.dp;
+  const Copy cw{w_rows, a.w_stride, count, a.features, to_w, l.dp, pw, 0, num->max_w, &num->of_w};
+  const Copy ch{h, a.h_stride, a.rows, a.features, to_h, l.dp, ph, masked, h_apart ? nullptr : num->max_h,
+                h_apart ? reinterpret_cast<float*>(ws + l.unit) : &num->of_h};
+  const unsigned first = w_direct ? 0 : grid_of(pw / 8, 4096), more = h_ready ? 0 : grid_of(ph / 8, 4096);
+  typedef typename std::conditional<NP == 1, uint16_t, float>::type T;
+  if (first + more) wino_launch((k_loss_planes<T, NP>), dim3(first + more), dim3(256), st, cw, ch, first, g);
+  *ow = w_direct ? Operand{(const uint16_t*)w_rows, a.w_stride, 0, 0, count, a.features}
+                 : Operand{to_w, l.dp, pw, 0, count, l.dp};
+  if (!h_ready) *oh = Operand{to_h, l.dp, ph, 0, a.rows, l.dp};
+}
+
 template <int NP>
 hipError_t forward(const LossArgs& a, const void* h, const void* w, const float* bias, const int64_t* target,
                    float* loss, float* lse, char* ws, hipStream_t st) {
-  typedef TileFor<NP> T;
   const LossLayout l = loss_layout(a, false);
-  Operand oh = direct(a, h, a.h_stride) ? Operand{(const uint16_t*)h, a.h_stride, 0, 0, a.rows}
-                                        : planes_of<NP>(a, h, a.h_stride, a.rows, ws + l.h, l.dp, st);
+  Numbers* num = reinterpret_cast<Numbers*>(ws + l.numbers);
   float2* best = reinterpret_cast<float2*>(ws + l.parts);
   float* hit = reinterpret_cast<float*>(ws + l.target);
-  const int tn = (a.rows + T::BN - 1) / T::BN;
-  const bool as_is = direct(a, w, a.w_stride);
+  const Rows g{target, a.ignore_index, a.rows, a.classes};
+  const bool w_direct = direct(a, w, a.w_stride);
+  bool h_ready = direct(a, h, a.h_stride);
+  Operand oh{(const uint16_t*)h, a.h_stride, 0, 0, a.rows, a.features}, ow{};
+  const int k = NP == 1 && a.features % 32 == 0 ? a.features : l.dp;
+  if (NP == 2)
+    wino_launch(k_loss_range, dim3(kRange), dim3(256), st, (const float*)w, a.w_stride, (const float*)nullptr, 0L,
+                a.features, g, (const float*)nullptr, num);
   // a launch holds fewer than 2^32 threads
-  const long most = (1L << 22) / tn < 2 ? 2 * kBM : (1L << 22) / tn * kBM;
-  const long piece = !as_is ? l.piece : a.classes < most ? a.classes : most;
-  Logits g{bias, target, a.ignore_index, a.rows, a.classes, 0, 0, l.dp};
+  const long most = (1L << 21) / ((a.rows + 63) / 64) * 64;
+  long piece = w_direct ? a.classes : l.piece;
+  if (piece > most) piece = most < 256 ? 256 : most / 256 * 256;
+  Logits q{bias, g, 0, 0, k, &num->of_w, reinterpret_cast<const float*>(ws + l.unit), 1};
   int part = 0;
   for (long first = 0; first < a.classes; first += piece) {
-    g.first = (int)first;
-    g.count = (int)(a.classes - first < piece ? a.classes - first : piece);
-    const void* rows = row_at(a, w, first, a.w_stride);
-    const Operand ow = as_is ? Operand{(const uint16_t*)rows, a.w_stride, 0, 0, g.count}
-                             : planes_of<NP>(a, rows, a.w_stride, g.count, ws + l.w, l.dp, st);
-    const int tm = (g.count + T::BM - 1) / T::BM;
-    wino_launch((k_loss_logits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, g, tm, tn, part, best, hit);
-    part += tm;
+    q.first = (int)first;
+    q.count = (int)(a.classes - first < piece ? a.classes - first : piece);
+    operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, NP == 2, false, num, ws, &ow,
+                 &oh, st);
+    h_ready = true;
+    with_tile<NP, false, false>(side_for(q.count, a.rows), [&](auto tile) {
+      typedef decltype(tile) T;
+      const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
+      wino_launch((k_loss_logits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, part, best, hit);
+      part += tm;
+    });
   }
-  wino_launch(k_loss_join, dim3((a.rows + 15) / 16), dim3(256), st, (const float2*)best, part, (const float*)hit, g,
-              loss, lse);
+  // few rows: all threads of a work group on one
+  if (a.rows >= 1024)
+    wino_launch((k_loss_join<16>), dim3((a.rows + 15) / 16), dim3(256), st, (const float2*)best, part, (const float*)hit,
+                g, loss, lse);
+  else
+    wino_launch((k_loss_join<256>), dim3(a.rows), dim3(256), st, (const float2*)best, part, (const float*)hit, g, loss,
+                lse);
   return hipGetLastError();
 }
 
@@ -453,56 +598,63 @@ template <int NP>
 hipError_t backward(const LossArgs& a, const void* h, const void* w, const float* bias, const int64_t* target,
                     const float* lse, const float* dloss, void* dh, void* dw, float* dbias, char* ws,
                     hipStream_t st) {
-  typedef TileFor<NP> T;
   const LossLayout l = loss_layout(a, true);
-  float* ref = reinterpret_cast<float*>(ws + l.ref);
-  Logits g{bias, target, a.ignore_index, a.rows, a.classes, 0, 0, l.dp};
-  wino_launch(k_loss_weight, dim3(1), dim3(1024), st, dloss, g, ref);
-  const Operand oh = direct(a, h, a.h_stride) ? Operand{(const uint16_t*)h, a.h_stride, 0, 0, a.rows}
-                                              : planes_of<NP>(a, h, a.h_stride, a.rows, ws + l.h, l.dp, st);
-  Operand ht{};
-  if (dw) ht = across<NP>(a, h, a.h_stride, a.rows, ws + l.ht, l.tp, target, st);
+  Numbers* num = reinterpret_cast<Numbers*>(ws + l.numbers);
+  const float* ref = &num->ref;
+  const Rows g{target, a.ignore_index, a.rows, a.classes};
+  wino_launch(k_loss_range, dim3(NP == 2 ? kRange : 1), dim3(256), st, NP == 2 ? (const float*)w : nullptr, a.w_stride,
+              NP == 2 ? (const float*)h : nullptr, a.h_stride, a.features, g, dloss, num);
+  const bool w_direct = direct(a, w, a.w_stride);
+  bool h_ready = false;   // always a copy: rows that are left out as zeros
+  Operand oh{}, ow{};
+  Logits q{bias, g, 0, 0, NP == 1 && a.features % 32 == 0 ? a.features : l.dp, &num->of_w, &num->of_h, 0};
   uint16_t* dl = reinterpret_cast<uint16_t*>(ws + l.dl);
-  uint16_t* dlt = reinterpret_cast<uint16_t*>(ws + l.dlt);
   float* db = dbias ? reinterpret_cast<float*>(ws + l.dbias) : nullptr;
   float* sums = reinterpret_cast<float*>(ws + l.dh);
-  const int tn = (int)((l.tp + T::BN - 1) / T::BN), td = (a.features + T::BM - 1) / T::BM;
-  const bool as_is = direct(a, w, a.w_stride);
   const bool one = l.splits == 1 && l.piece >= a.classes;   // dh comes from one product
+  int parts = 0;
   for (long first = 0; first < a.classes; first += l.piece) {
-    g.first = (int)first;
-    g.count = a.classes - g.first < l.piece ? a.classes - g.first : l.piece;
-    const int vp = (int)up(g.count, 64);
-    const void* rows = row_at(a, w, first, a.w_stride);
-    const Operand ow = as_is ? Operand{(const uint16_t*)rows, a.w_stride, 0, 0, g.count}
-                             : planes_of<NP>(a, rows, a.w_stride, g.count, ws + l.w, l.dp, st);
-    const int tm = (vp + T::BM - 1) / T::BM;
-    const long dl_plane = (long)a.rows * vp, dlt_plane = (long)g.count * l.tp;
-    wino_launch((k_loss_dlogits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, g, tm, tn, lse, dloss,
-                (const float*)ref, dl, (long)vp, dl_plane, dlt, (long)l.tp, dlt_plane, db);
+    q.first = (int)first;
+    q.count = a.classes - q.first < l.piece ? a.classes - q.first : l.piece;
+    const int vp = (int)up(q.count, 64);
+    operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, true, num, ws, &ow, &oh,
+                 st);
+    h_ready = true;
+    const long plane = (long)a.rows * vp;
+    with_tile<NP, false, false>(l.side, [&](auto tile) {
+      typedef decltype(tile) T;
+      const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
+      parts = tn * T::WN;
+      wino_launch((k_loss_dlogits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, lse, dloss, ref, dl, vp,
+                  plane, db);
+    });
+    const Operand od{dl, vp, plane, 0, a.rows, vp};
     if (dh) {
-      const Operand wt = across<NP>(a, rows, a.w_stride, g.count, ws + l.wt, vp, nullptr, st);
-      const Operand od{dl, vp, dl_plane, 0, a.rows};
       const int per = (int)up((vp + l.splits - 1) / l.splits, 64);
       Product p{one ? dh : (void*)sums, a.features, (long)a.rows * a.features, one ? a.bf16 : first ? 3 : 2, vp, per,
-                ref};
-      const int t = (a.rows + T::BN - 1) / T::BN;
-      wino_launch((k_loss_product<T>), dim3(td * t, l.splits), dim3(T::THREADS), st, wt, od, p, td, t);
+                a.features, a.rows, ref, &num->of_w};
+      with_tile<NP, true, false>(l.dh_side, [&](auto tile) {
+        typedef decltype(tile) T;
+        const int tm = (a.features + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
+        wino_launch((k_loss_product<T>), dim3(tm * tn, l.splits), dim3(T::THREADS), st, ow, od, p, tm, tn);
+      });
     }
     if (dw) {
-      const Operand od{dlt, l.tp, dlt_plane, 0, g.count};
-      Product p{const_cast<void*>(row_at(a, dw, first, a.features)), a.features, 0, a.bf16, l.tp, l.tp, ref};
-      const int t = (g.count + T::BN - 1) / T::BN;
-      wino_launch((k_loss_product<T>), dim3(td * t), dim3(T::THREADS), st, ht, od, p, td, t);
+      const int tk = (int)up(a.rows, 32);
+      Product p{const_cast<void*>(row_at(a, dw, first, a.features)), a.features, 0, a.bf16, tk, tk, a.features, q.count,
+                ref, &num->of_h};
+      with_tile<NP, true, true>(side_for(a.features, q.count), [&](auto tile) {
+        typedef decltype(tile) T;
+        const int tm = (a.features + T::BM - 1) / T::BM, tn = (q.count + T::BN - 1) / T::BN;
+        wino_launch((k_loss_product<T>), dim3(tm * tn), dim3(T::THREADS), st, oh, od, p, tm, tn);
+      });
     }
   }
   const long items = (long)a.rows * a.features;
-  if (dh && !one)
-    wino_launch(k_loss_sums, dim3(grid_of(items)), dim3(256), st, (const float*)sums, l.splits, items, items, a.bf16,
-                (const float*)ref, dh);
-  if (dbias)
-    wino_launch(k_loss_dbias, dim3((a.classes + 255) / 256), dim3(256), st, (const float*)db, tn * T::WN, a.classes,
-                (const float*)ref, dbias);
+  const unsigned first = dh && !one ? grid_of(items, 8192) : 0, more = dbias ? grid_of(a.classes, 1024) : 0;
+  if (first + more)
+    wino_launch(k_loss_sums, dim3(first + more), dim3(256), st, (const float*)sums, l.splits, items, a.bf16, dh, first,
+                (const float*)db, parts, a.classes, dbias, ref);
   return hipGetLastError();
 }
 
@@ -511,50 +663,49 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
 LossLayout loss_layout(const LossArgs& a, bool back) {
   LossLayout l{};
   const size_t T = (size_t)a.rows, D = (size_t)a.features, V = (size_t)a.classes;
-  l.planes = a.bf16 ? 1 : 3;
-  const size_t item = 2 * (size_t)l.planes;   // bytes of a value in planes
+  const int np = a.bf16 ? 1 : 2;
+  const size_t item = 2 * (size_t)np;   // bytes of a value in planes
   l.dp = (int)up(D, 64);
-  l.tp = (int)up(T, 64);
-  // classes per piece: what the caller asks for, or as many as keep a piece's dl and weights, both
-  // as rows and as columns, within 256 MiB
-  size_t piece = a.piece ? (size_t)a.piece : ((size_t)256 << 20) / (2 * item * ((size_t)l.tp + l.dp));
+  // classes per piece: what the caller asks for, or as many as keep a piece's dl and planes of W within
+  // 256 MiB
+  size_t piece = a.piece ? (size_t)a.piece : ((size_t)256 << 20) / (item * (T + l.dp));
   piece = up(piece < 1024 && !a.piece ? 1024 : piece, 256);
   if (piece > (size_t)kMaxLd) piece = (size_t)kMaxLd;
   l.piece = (int)(piece < V ? piece : V);
   const size_t P = (size_t)l.piece, vp = up(P, 64);
   size_t at = 0;
   const auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
+  l.numbers = take(sizeof(Numbers));
   l.w = take(item * P * l.dp);
   l.h = take(item * T * l.dp);
+  l.splits = 1;
   if (!back) {
-    // a tile of classes never spans two pieces
-    const size_t pieces = (V + P - 1) / P;
-    l.parts = take(8 * T * (pieces * ((P + kBM - 1) / kBM) + (V + kBM - 1) / kBM));
+    // pieces are whole multiples of 256 classes, so no tile spans two
+    const size_t least = T >= 160 * 256 ? 256 : T >= 160 * 128 ? 128 : 64;   // of side_for() for any classes
+    l.parts = take(8 * T * (up(V, 256) / least));
     l.target = take(4 * T);
-    l.splits = 1;
+    l.unit = take(4 * T);
   } else {
-    l.ref = take(4);
-    l.ht = take(item * D * l.tp);
-    l.wt = take(item * D * vp);
     l.dl = take(item * T * vp);
-    l.dlt = take(item * P * l.tp);
+    l.side = side_for((long)P, (long)T);
     // ranges of classes until dh's tiles fill the chip, each of 512 classes or more
-    const size_t tiles = ((D + kBM - 1) / kBM) * ((T + kBN - 1) / kBN);
-    size_t s = tiles ? (256 + tiles - 1) / tiles : 1;
-    if (s > vp / 512) s = vp / 512;
-    if (s < 1) s = 1;
-    l.splits = (int)s;
-    l.dh = take(4 * T * D * s);
-    l.dbias = take(4 * V * kWN * ((l.tp + kBN - 1) / kBN));
+    const long room = (long)(vp / 512 ? vp / 512 : 1);
+    l.dh_side = side_for((long)D, (long)T, room < 8 ? room : 8);
+    const long tiles = T ? count_of((long)D, (long)T, l.dh_side) : 1;
+    long s = (256 + tiles - 1) / tiles;
+    if (s > room) s = room;
+    l.splits = (int)(s < 1 ? 1 : s);
+    l.dh = take(4 * T * D * l.splits);
+    l.dbias = take(4 * V * waves_n(l.side, np) * (T ? (T + l.side - 1) / l.side : 1));
   }
-  l.bytes = at ? at : 256;
+  l.bytes = at;
   return l;
 }
 
 hipError_t launch_loss(const LossArgs& a, const void* h, const void* w, const float* bias,
                        const int64_t* target, float* loss, float* lse, char* ws, hipStream_t st) {
   return a.bf16 ? forward<1>(a, h, w, bias, target, loss, lse, ws, st)
-                : forward<3>(a, h, w, bias, target, loss, lse, ws, st);
+                : forward<2>(a, h, w, bias, target, loss, lse, ws, st);
 }
 
 hipError_t launch_loss_backward(const LossArgs& a, const void* h, const void* w, const float* bias,
@@ -562,13 +713,13 @@ hipError_t launch_loss_backward(const LossArgs& a, const void* h, const void* w,
                                 void* dw, float* dbias, char* ws, hipStream_t st) {
   if (a.rows == 0) {   // no rows: the weights' gradient is zero
     const long items = (long)a.classes * a.features * (a.bf16 ? 1 : 2);
-    if (dw) wino_launch(k_loss_zero, dim3(grid_of(items)), dim3(256), st, (uint16_t*)dw, items);
+    if (dw) wino_launch(k_loss_zero, dim3(grid_of(items, 16384)), dim3(256), st, (uint16_t*)dw, items);
     if (dbias)
-      wino_launch(k_loss_zero, dim3(grid_of(2L * a.classes)), dim3(256), st, (uint16_t*)dbias, 2L * a.classes);
+      wino_launch(k_loss_zero, dim3(grid_of(2L * a.classes, 16384)), dim3(256), st, (uint16_t*)dbias, 2L * a.classes);
     return hipGetLastError();
   }
   return a.bf16 ? backward<1>(a, h, w, bias, target, lse, dloss, dh, dw, dbias, ws, st)
-                : backward<3>(a, h, w, bias, target, lse, dloss, dh, dw, dbias, ws, st);
+                : backward<2>(a, h, w, bias, target, lse, dloss, dh, dw, dbias, ws, st);
 }
 
 }  // namespace wino

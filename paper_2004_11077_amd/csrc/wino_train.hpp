@@ -35,10 +35,10 @@ struct LossArgs {
 };
 // Regions of the workspace, bytes from its start; `bytes` in all.
 struct LossLayout {
-  int planes;             // bf16 planes of an operand
-  int piece, dp, tp;      // classes per piece; features, rows rounded up to whole stages
-  int splits;             // of the classes of a piece in dh's product
-  size_t w, h, parts, target, ref, ht, wt, dl, dlt, dh, dbias, bytes;
+  int piece, dp;          // classes per piece; features rounded up to whole lines
+  int side, dh_side;      // tiles of dl's and dh's products
+  int splits;             // ranges of the classes of a piece in dh's product
+  size_t numbers, w, h, parts, target, unit, dl, dh, dbias, bytes;
 };
 LossLayout loss_layout(const LossArgs& a, bool backward);
 hipError_t launch_loss(const LossArgs& a, const void* h, const void* w, const float* bias,
@@ -54,9 +54,9 @@ struct UpdateArgs {
   long g_batch, g_stride, o_batch, o_stride;
 };
 struct UpdateLayout {
-  int r, c, rp, cp;           // r <= c: the smaller and the larger side; rounded up to whole blocks of k
+  int r, c, rp, cp;           // r <= c: the smaller and the larger side; rounded up to whole lines
   int splits;                 // ranges of k of A's product
-  size_t norms, x, xt, x2, xt2, gram, poly, parts, bytes;
+  size_t norms, x, x2, gram, poly, parts, bytes;
 };
 UpdateLayout update_layout(const UpdateArgs& a);
 hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, hipStream_t st);

@@ -2,12 +2,11 @@
 //
 //   X = G / (|G|_F + eps);  `steps` times  A = X X^T,  X <- a X + (b A + c A A) X;  O = scale X
 //
-// on the smaller side's products (a taller matrix is taken across).  Three products a step, each with
-// its k contiguous in both operands (wino_products.hpp): A from X, the polynomial P = a I + b A + c A A
-// from A, which is symmetric, and the new X from P and X across.  Every product leaves its result cut
-// into the two fp16 planes that the next one takes, blocked as the instruction reads them, the new X
-// both ways.  A step multiplies small singular values by a and the errors of earlier steps with them,
-// by 3.4^4 in all for the usual coefficients, so bf16 results need the second plane as well.
+// on the smaller side's products (a taller matrix is taken across).  Three products a step
+// (wino_products.hpp): A = X X^T, the polynomial P = a I + b A + c A A from A, which is symmetric, and
+// the new X = P X.  Every product leaves its result cut into the two fp16 planes that the next one
+// takes.  A step multiplies small singular values by a and the errors of earlier steps with them, by
+// 3.4^4 in all for the usual coefficients, so bf16 results need the second plane as well.
 //
 // Powers of two that bring X, A and P into fp16's range are known on the host: no singular value of X
 // exceeds one at first, nor, after a step, the largest |a s + b s^3 + c s^5| of those before it, and no
@@ -22,7 +21,7 @@ namespace {
 
 using namespace prod;
 
-constexpr int kNormParts = 64;
+constexpr int kNormParts = 256;
 
 __device__ __forceinline__ float value(const void* p, long i, int bf16) {
   return bf16 ? bf16_value(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
@@ -32,12 +31,19 @@ __device__ __forceinline__ float value(const void* p, long i, int bf16) {
 __global__ __launch_bounds__(256) void k_update_norm(const void* __restrict__ g, UpdateArgs a,
                                                      double* __restrict__ norms) {
   __shared__ double lds[4];
-  const long base = blockIdx.y * a.g_batch, items = (long)a.rows * a.cols;
+  const long base = blockIdx.y * a.g_batch;
   double s = 0;
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += kNormParts * 256) {
-    const long r = i / a.cols;
-    const double v = value(g, base + r * a.g_stride + (i - r * a.cols), a.g_bf16);
+  const auto take = [&](long at) {
+    const double v = value(g, base + at, a.g_bf16);
     s += v * v;
+  };
+  if (a.g_stride == a.cols) {   // one run of values
+    const long items = (long)a.rows * a.cols;
+#pragma unroll 8
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += kNormParts * 256) take(i);
+  } else {
+    for (int r = blockIdx.x; r < a.rows; r += kNormParts)
+      for (int c = threadIdx.x; c < a.cols; c += 256) take(r * a.g_stride + c);
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d, 64);
@@ -46,18 +52,17 @@ __global__ __launch_bounds__(256) void k_update_norm(const void* __restrict__ g,
   if (threadIdx.x == 0) norms[blockIdx.y * kNormParts + blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
-// fp16 planes of a matrix, blocked: rows of kb blocks of 32; 2^e times the values.
+// fp16 planes of a matrix, rows of ld elements (whole lines, zeros behind the matrix); 2^e times the
+// values.
 struct Planes {
   uint16_t* p;
   long plane, batch;
-  int kb, e;
+  int ld, e;
 };
 
-__device__ __forceinline__ float power(int e) { return __builtin_ldexpf(1.f, e); }
-
-// Four consecutive k of a row, from a multiple of four.
+// Four consecutive elements of a row, from a multiple of four.
 __device__ __forceinline__ void put(const Planes& o, int row, int k, f32x4 v) {
-  uint16_t* to = o.p + blockIdx.z * o.batch + blocked(row, k, o.kb);
+  uint16_t* to = o.p + blockIdx.z * o.batch + (long)row * o.ld + k;
   const float s = power(o.e);
   uint16_t q[4][2];
 #pragma unroll
@@ -66,37 +71,34 @@ __device__ __forceinline__ void put(const Planes& o, int row, int k, f32x4 v) {
   for (int p = 0; p < 2; ++p)
     *reinterpret_cast<ushort4*>(to + p * o.plane) = make_ushort4(q[0][p], q[1][p], q[2][p], q[3][p]);
 }
-// The same four values as one k of four consecutive rows, from a multiple of four.
+// The same four values as one element of four consecutive rows.
 __device__ __forceinline__ void put_across(const Planes& o, int row, int k, int rows, f32x4 v) {
-  uint16_t* to = o.p + blockIdx.z * o.batch + blocked(row, k, o.kb);
+  uint16_t* to = o.p + blockIdx.z * o.batch + (long)row * o.ld + k;
   const float s = power(o.e);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if (row + e >= rows) continue;
     uint16_t q[2];
     cut<2>(v[e] * s, q);
-    to[e * 8] = q[0];
-    to[o.plane + e * 8] = q[1];
+    to[(long)e * o.ld] = q[0];
+    to[o.plane + (long)e * o.ld] = q[1];
   }
 }
 
-// G -> X, both ways: 64 x 64 values a work group.
+// G -> X: 64 x 64 values a work group.
 __global__ __launch_bounds__(256) void k_update_planes(const void* __restrict__ g, UpdateArgs a, int r, int c,
-                                                       int across, const double* __restrict__ norms, Planes x,
-                                                       Planes xt) {
+                                                       int across, const double* __restrict__ norms, Planes x) {
   __shared__ float tile[64][65];
-  __shared__ double total;
-  if (threadIdx.x < 64) {
-    double s = norms[blockIdx.z * kNormParts + threadIdx.x];
+  __shared__ double sums[4];
+  double s = norms[blockIdx.z * kNormParts + threadIdx.x];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d, 64);
-    if (threadIdx.x == 0) total = s;
-  }
+  for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d, 64);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
   __syncthreads();
-  const double inv = 1.0 / (__builtin_sqrt(total) + (double)a.eps);
+  const double inv = 1.0 / (__builtin_sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + (double)a.eps);
   const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;   // of X
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll 4
+#pragma unroll 8
   for (int i = 0; i < 16; ++i) {
     // lanes along the rows of G
     const int q = wave + i * 4, rr = across ? r0 + lane : r0 + q, cc = across ? c0 + q : c0 + lane;
@@ -109,33 +111,29 @@ __global__ __launch_bounds__(256) void k_update_planes(const void* __restrict__ 
     else tile[q][lane] = v;
   }
   __syncthreads();
-  // 16 blocks of 16 x 32, eight of X and eight of X across; a lane's eight values are one store
+  const float unit = power(x.e);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int block = wave + i * 4, way = block >> 3, q = block & 7;
-    const int row = (q >> 1) * 16 + (lane & 15), k = (q & 1) * 32 + (lane >> 4) * 8;
-    const Planes& o = way ? xt : x;
-    const int row_at = (way ? c0 : r0) + row, k_at = (way ? r0 : c0) + k;
-    if ((row_at & ~15) >= (way ? c : r) || k_at >= o.kb * 32) continue;
-    const float s = power(o.e);
+  for (int i = 0; i < 2; ++i) {
+    const int row = (threadIdx.x >> 3) + i * 32, k = (threadIdx.x & 7) * 8;
+    if (r0 + row >= r) continue;
     __attribute__((aligned(16))) uint16_t out[2][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       uint16_t h[2];
-      cut<2>((way ? tile[k + e][row] : tile[row][k + e]) * s, h);
+      cut<2>(tile[row][k + e] * unit, h);
       out[0][e] = h[0];
       out[1][e] = h[1];
     }
-    uint16_t* to = o.p + blockIdx.z * o.batch + blocked(row_at, k_at, o.kb);
+    uint16_t* to = x.p + blockIdx.z * x.batch + (long)(r0 + row) * x.ld + c0 + k;
     *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(out[0]);
-    *reinterpret_cast<uint4*>(to + o.plane) = *reinterpret_cast<const uint4*>(out[1]);
+    *reinterpret_cast<uint4*>(to + x.plane) = *reinterpret_cast<const uint4*>(out[1]);
   }
 }
 
-// What becomes of the products.  kGram: A.  kPoly: P.  kNext: X both ways.  kLast: the result.
+// What becomes of the products.  kGram: A.  kPoly: P.  kNext: X.  kLast: the result.
 enum Kind { kGram, kPoly, kNext, kLast };
 struct Result {
-  Planes out, out_t;      // kGram, kPoly: out; kNext: X and X across
+  Planes out;             // of A, P or X
   Planes gram;            // kPoly: A
   int r, c;               // sides of X
   int e;                  // exponents of the two operands, added
@@ -145,9 +143,9 @@ struct Result {
   long o_batch, o_stride;
 };
 
-// Four values D[m .. m + 3][n] of a product of batch blockIdx.z: m is a row of the first operand and
-// becomes k of the result's row n.  kGram, kPoly: `mirror` writes row m, k n as well.  Elements of k
-// beyond the matrix, up to whole blocks, become zeros: the next product multiplies them.
+// Four values D[m .. m + 3][n] of a product of batch blockIdx.z: elements m of the result's row n.
+// kGram, kPoly: `mirror` writes element n of rows m .. m + 3 as well.  Elements behind the matrix, up to
+// whole lines, become zeros: the next product multiplies them.
 template <Kind KIND>
 __device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, bool mirror) {
   const float unit = power(-s.e);
@@ -155,8 +153,8 @@ __device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, b
   for (int e = 0; e < 4; ++e) v[e] *= unit;
   const int km = KIND <= kPoly ? s.r : s.c;   // rows of the first operand
   if constexpr (KIND == kPoly) {
-    if (n < s.r && m < s.gram.kb * 32) {
-      const uint16_t* at = s.gram.p + blockIdx.z * s.gram.batch + blocked(n, m, s.gram.kb);
+    if (n < s.r && m < s.gram.ld) {
+      const uint16_t* at = s.gram.p + blockIdx.z * s.gram.batch + (long)n * s.gram.ld + m;
       const ushort4 h = *reinterpret_cast<const ushort4*>(at), l = *reinterpret_cast<const ushort4*>(at + s.gram.plane);
       const float one = power(-s.gram.e);
       const float old[4] = {f16_value(h.x) + f16_value(l.x), f16_value(h.y) + f16_value(l.y),
@@ -180,12 +178,9 @@ __device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, b
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (m + e >= km) k[e] = 0;
-    if (n < s.r && m < s.out.kb * 32) put(s.out, n, m, k);
-    if (KIND == kNext || mirror) {
-      const Planes& t = KIND == kNext ? s.out_t : s.out;
-      if (n >= s.r) v = f32x4{0, 0, 0, 0};
-      if (n < t.kb * 32) put_across(t, m, n, km, v);
-    }
+    if (n < s.r && m < s.out.ld) put(s.out, n, m, k);
+    // zeros behind a row of the mirror image come from the tile that holds them unmirrored
+    if (KIND <= kPoly && mirror && n < s.r) put_across(s.out, m, n, s.r, v);
   }
 }
 
@@ -209,7 +204,7 @@ __global__ __launch_bounds__(T::THREADS) void k_update_product(Operand x, Operan
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   const int k0 = blockIdx.y * per, k1 = k0 + per < k ? k0 + per : k;
   f32x4 acc[T::TM][T::TN] = {};
-  multiply<T>(x, y, blockIdx.z, m0, n0, k0, k1, k, lds, acc);
+  multiply<T>(x, y, blockIdx.z, m0, n0, k0, k1, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
 #pragma unroll
@@ -246,44 +241,45 @@ __global__ __launch_bounds__(256) void k_update_join(const float* __restrict__ p
   }
 }
 
-// Products of few tiles, where waiting counts: 32 x 32 of D a wave, fragments straight from memory
-// into registers, no barrier in the loop.  SHARE: the four waves of a work group take every fourth
-// block of k and join their sums in LDS; otherwise they are 2 x 2 over a tile of 64 x 64.
-template <bool SHARE, Kind KIND>
+// Products of few tiles and k along the rows of both operands, where waiting counts: 32 x 32 of D a
+// work group, whose four waves take every fourth block of k, fragments straight from memory into
+// registers, no barrier in the loop; their sums are joined in LDS.
+template <Kind KIND>
 __global__ __launch_bounds__(256) void k_update_few(Operand x, Operand y, int k, int tiles_m, Result s) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int SIDE = SHARE ? 32 : 64, DEPTH = 4;
+  constexpr int DEPTH = 4;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m0 = blockIdx.x % tiles_m * SIDE + (SHARE ? 0 : (wave & 1) * 32);
-  const int n0 = blockIdx.x / tiles_m * SIDE + (SHARE ? 0 : (wave >> 1) * 32);
-  if (!SHARE && (m0 >= x.rows || n0 >= y.rows)) return;   // nothing there, not even zeros to write
+  const int m0 = blockIdx.x % tiles_m * 32, n0 = blockIdx.x / tiles_m * 32;
   __amdgpu_buffer_rsrc_t rx[2], ry[2];
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
-    rx[q] = rows_of<true>(x, q, blockIdx.z, m0, 32, k);
-    ry[q] = rows_of<true>(y, q, blockIdx.z, n0, 32, k);
+    const int left_x = x.rows - m0 < 32 ? x.rows - m0 : 32, left_y = y.rows - n0 < 32 ? y.rows - n0 : 32;
+    rx[q] = window(x.p + q * x.plane + blockIdx.z * x.batch + (long)m0 * x.ld, left_x * x.ld * 2);
+    ry[q] = window(y.p + q * y.plane + blockIdx.z * y.batch + (long)n0 * y.ld, left_y * y.ld * 2);
   }
-  const int at[4] = {lane * 16, (int)x.ld * 2 + lane * 16, lane * 16, (int)y.ld * 2 + lane * 16};
+  const int ax = ((lane & 15) * (int)x.ld + (lane >> 4) * 8) * 2, ay = ((lane & 15) * (int)y.ld + (lane >> 4) * 8) * 2;
+  const int at_x[2] = {ax, ax + 32 * (int)x.ld}, at_y[2] = {ay, ay + 32 * (int)y.ld};
   f32x4 acc[2][2] = {};
-  const int blocks = k / 32, first = SHARE ? wave : 0, step = SHARE ? 4 : 1;
-  for (int b = first; b < blocks; b += DEPTH * step) {
+  const int blocks = k / 32;
+  for (int b = wave; b < blocks; b += DEPTH * 4) {
     u32x4 fx[DEPTH][2][2], fy[DEPTH][2][2];
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
-      // beyond the last block: any block, multiplied by nothing
-      const int to = (b + d * step < blocks ? b + d * step : b) * 1024;
+      // beyond the last block: any block, and not multiplied
+      const int to = (b + d * 4 < blocks ? b + d * 4 : b) * 64;
 #pragma unroll
       for (int q = 0; q < 2; ++q)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          fx[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx[q], at[i], to, 0));
-          fy[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry[q], at[2 + i], to, 0));
+          fx[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx[q], at_x[i], to, 0));
+          fy[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry[q], at_y[i], to, 0));
         }
     }
+    __builtin_amdgcn_sched_barrier(0);   // all loads first
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
-      if (b + d * step >= blocks) break;
+      if (b + d * 4 >= blocks) break;
 #pragma unroll
       for (int t = 1; t >= 0; --t)
 #pragma unroll
@@ -294,63 +290,63 @@ __global__ __launch_bounds__(256) void k_update_few(Operand x, Operand y, int k,
             for (int j = 0; j < 2; ++j) acc[i][j] = multiply_block<2>(fx[d][q][i], fy[d][t - q][j], acc[i][j]);
     }
   }
-  if constexpr (SHARE) {
-    __shared__ f32x4 join[4][4][64];
+  __shared__ f32x4 join[4][4][64];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) join[wave][i * 2 + j][lane] = acc[i][j];
-    __syncthreads();
-    // one of the four 16 x 16 blocks a wave
-    f32x4 v = join[0][wave][lane];
+    for (int j = 0; j < 2; ++j) join[wave][i * 2 + j][lane] = acc[i][j];
+  __syncthreads();
+  // one of the four 16 x 16 blocks a wave
+  f32x4 v = join[0][wave][lane];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) v += join[w][wave][lane];
-    finish<KIND>(s, m0 + (wave >> 1) * 16 + (lane >> 4) * 4, n0 + (wave & 1) * 16 + (lane & 15), v, false);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        finish<KIND>(s, m0 + i * 16 + (lane >> 4) * 4, n0 + j * 16 + (lane & 15), acc[i][j], false);
-  }
+  for (int w = 1; w < 4; ++w) v += join[w][wave][lane];
+  finish<KIND>(s, m0 + (wave >> 1) * 16 + (lane >> 4) * 4, n0 + (wave & 1) * 16 + (lane & 15), v, false);
 #endif
 }
 
-typedef Tile<128, 128, 2, 4, 2, 4, true> Mid;
+// Tiles of products; AX: k across the rows of the first operand (X in P X).
+template <bool AX>
+struct Tiles {
+  typedef Tile<256, 256, 2, 4, 2, 2, AX> Big;
+  typedef Tile<128, 128, 2, 4, 2, 4, AX> Mid;
+  typedef Tile<64, 64, 2, 2, 2, 4, AX> Small;
+};
 
 int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
 int half_of(int tiles) { return tiles * (tiles + 1) / 2; }
 
-// Few rows: the products' tiles of 128 would leave most of the chip idle.
+// Few rows: the symmetric products' tiles of 128 would leave most of the chip idle.
 bool few(const UpdateLayout& l, int batch) { return (long)l.r * l.r * batch <= 256L * 256 * 4; }
 
 template <Kind KIND>
 void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& y, int k, const Result& s,
              float* parts, hipStream_t st) {
-  const int rows_m = KIND <= kPoly ? l.r : l.c, rows_n = l.r;
-  if (few(l, batch)) {
-    if (k >= 512) {
-      const int tm = tiles_of(rows_m, 32);
-      wino_launch((k_update_few<true, KIND>), dim3(tm * tiles_of(rows_n, 32), 1, batch), dim3(256), st, x, y, k, tm, s);
-    } else {
-      const int tm = tiles_of(rows_m, 64);
-      wino_launch((k_update_few<false, KIND>), dim3(tm * tiles_of(rows_n, 64), 1, batch), dim3(256), st, x, y, k, tm,
-                  s);
+  if constexpr (KIND <= kPoly) {
+    if (few(l, batch)) {
+      const int tm = tiles_of(l.r, 32);
+      wino_launch((k_update_few<KIND>), dim3(tm * tm, 1, batch), dim3(256), st, x, y, k, tm, s);
+      return;
     }
-    return;
-  }
-  const int tm = tiles_of(rows_m, 128), tn = tiles_of(rows_n, 128);
-  if constexpr (KIND == kGram) {
-    const int tiles = half_of(tm), per = (int)up((k + l.splits - 1) / l.splits, 32);
+    typedef Tiles<false>::Mid T;
+    const int tm = tiles_of(l.r, T::BM), splits = KIND == kGram ? l.splits : 1;
+    const int per = (int)up((k + splits - 1) / splits, 32);
     const long part = (long)batch * l.r * l.rp;
-    wino_launch((k_update_product<Mid, KIND>), dim3(tiles, l.splits, batch), dim3(Mid::THREADS), st, x, y, k, per, tm,
-                s, l.splits > 1 ? parts : nullptr, part, l.rp);
-    if (l.splits > 1)
+    wino_launch((k_update_product<T, KIND>), dim3(half_of(tm), splits, batch), dim3(T::THREADS), st, x, y, k, per, tm, s,
+                splits > 1 ? parts : nullptr, part, l.rp);
+    if (splits > 1)
       wino_launch((k_update_join<KIND>), dim3(half_of(tiles_of(l.rp, 64)), 1, batch), dim3(256), st,
-                  (const float*)parts, l.splits, part, l.rp, s);
+                  (const float*)parts, splits, part, l.rp, s);
   } else {
-    wino_launch((k_update_product<Mid, KIND>), dim3(KIND == kPoly ? half_of(tm) : tm * tn, 1, batch),
-                dim3(Mid::THREADS), st, x, y, k, k, tm, s, (float*)nullptr, 0L, 0);
+    const auto go = [&](auto tile) {
+      typedef decltype(tile) T;
+      const int tm = tiles_of(l.c, T::BM), tn = tiles_of(l.r, T::BN);
+      wino_launch((k_update_product<T, KIND>), dim3(tm * tn, 1, batch), dim3(T::THREADS), st, x, y, k, k, tm, s,
+                  (float*)nullptr, 0L, 0);
+    };
+    const auto count = [&](int side) { return (long)tiles_of(l.c, side) * tiles_of(l.r, side) * batch; };
+    if (count(256) >= 128) go(Tiles<true>::Big{});
+    else if (count(128) >= 128) go(Tiles<true>::Mid{});
+    else go(Tiles<true>::Small{});
   }
 }
 
@@ -369,18 +365,16 @@ UpdateLayout update_layout(const UpdateArgs& a) {
   UpdateLayout l{};
   l.r = a.rows < a.cols ? a.rows : a.cols;
   l.c = a.rows < a.cols ? a.cols : a.rows;
-  l.rp = (int)up(l.r, 32);
-  l.cp = (int)up(l.c, 32);
+  l.rp = (int)up(l.r, 64);
+  l.cp = (int)up(l.c, 64);
   size_t at = 0;
   const auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
-  const size_t r16 = up(l.r, 16), c16 = up(l.c, 16), item = 2 * 2 * (size_t)a.batch;   // two planes
+  const size_t item = 2 * 2 * (size_t)a.batch;   // two planes
   l.norms = take(sizeof(double) * kNormParts * a.batch);
-  l.x = take(item * r16 * l.cp);
-  l.xt = take(item * c16 * l.rp);
-  l.x2 = take(item * r16 * l.cp);
-  l.xt2 = take(item * c16 * l.rp);
-  l.gram = take(item * r16 * l.rp);
-  l.poly = take(item * r16 * l.rp);
+  l.x = take(item * l.r * l.cp);
+  l.x2 = take(item * l.r * l.cp);
+  l.gram = take(item * l.r * l.rp);
+  l.poly = take(item * l.r * l.rp);
   l.splits = 1;
   if (a.batch && l.r && !few(l, a.batch)) {
     // ranges of A's k until its tiles fill the chip, each of 256 or more
@@ -399,17 +393,18 @@ hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, 
   const int across = a.rows > a.cols;
   double* norms = reinterpret_cast<double*>(ws + l.norms);
   wino_launch(k_update_norm, dim3(kNormParts, a.batch), dim3(256), st, g, a, norms);
-  const long r16 = (long)up(l.r, 16), c16 = (long)up(l.c, 16);
-  const auto planes = [&](size_t at, long rows, int k, int e) {
-    return Planes{reinterpret_cast<uint16_t*>(ws + at), rows * k * a.batch, rows * k, k / 32, e};
+  const auto planes = [&](size_t at, int ld, int e) {
+    const long items = (long)l.r * ld;
+    return Planes{reinterpret_cast<uint16_t*>(ws + at), items * a.batch, items, ld, e};
   };
-  const auto operand = [](const Planes& p, long rows) { return Operand{p.p, p.kb * 512L, p.plane, p.batch, (int)rows}; };
+  const auto operand = [&](const Planes& p) { return Operand{p.p, p.ld, p.plane, p.batch, l.r, p.ld}; };
   // largest singular value that X can have
   double s = 1;
-  Planes x = planes(l.x, r16, l.cp, exponent(s)), xt = planes(l.xt, c16, l.rp, exponent(s));
-  wino_launch(k_update_planes, dim3((l.cp + 63) / 64, (l.rp + 63) / 64, a.batch), dim3(256), st, g, a, l.r, l.c, across,
-              (const double*)norms, x, xt);
+  Planes x = planes(l.x, l.cp, exponent(s));
+  wino_launch(k_update_planes, dim3(l.cp / 64, l.rp / 64, a.batch), dim3(256), st, g, a, l.r, l.c, across,
+              (const double*)norms, x);
   float* parts = reinterpret_cast<float*>(ws + l.parts);
+  const int rk = (int)up(l.r, 32);
   for (int i = 0; i < a.steps; ++i) {
     // largest |p(t)|, p(t) = a + b t + c t^2 on [0, s^2], and largest s |p(s^2)|: at the ends or where
     // the derivative vanishes
@@ -430,23 +425,22 @@ hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, 
     } else if (B != 0) {
       at(-A / (3 * B));
     }
-    const Planes gram = planes(l.gram, r16, l.rp, exponent(end)), poly = planes(l.poly, r16, l.rp, exponent(most_p));
+    const Planes gram = planes(l.gram, l.rp, exponent(end)), poly = planes(l.poly, l.rp, exponent(most_p));
     Result q{};
     q.r = l.r, q.c = l.c, q.a = a.a, q.b = a.b, q.c2 = a.c, q.scale = a.scale;
     q.across = across, q.bf16 = a.o_bf16, q.o = o, q.o_batch = a.o_batch, q.o_stride = a.o_stride;
     q.out = gram, q.e = 2 * x.e;
-    product<kGram>(l, a.batch, operand(x, l.r), operand(x, l.r), l.cp, q, parts, st);
+    product<kGram>(l, a.batch, operand(x), operand(x), (int)up(l.c, 32), q, parts, st);
     q.out = poly, q.gram = gram, q.e = 2 * gram.e;
-    product<kPoly>(l, a.batch, operand(gram, l.r), operand(gram, l.r), l.rp, q, parts, st);
+    product<kPoly>(l, a.batch, operand(gram), operand(gram), rk, q, parts, st);
     // Room for the products' roundings, and no more: the usual coefficients keep [0, 1.26] within
     // itself, from 1.27 on every step would enlarge it.
     s = 1.0001 * most_x;
-    const bool odd = i & 1;
-    const Planes x2 = planes(odd ? l.x : l.x2, r16, l.cp, exponent(s)), xt2 = planes(odd ? l.xt : l.xt2, c16, l.rp, exponent(s));
-    q.out = x2, q.out_t = xt2, q.e = xt.e + poly.e;
-    if (i + 1 < a.steps) product<kNext>(l, a.batch, operand(xt, l.c), operand(poly, l.r), l.rp, q, parts, st);
-    else product<kLast>(l, a.batch, operand(xt, l.c), operand(poly, l.r), l.rp, q, parts, st);
-    x = x2, xt = xt2;
+    const Planes next = planes(i & 1 ? l.x : l.x2, l.cp, exponent(s));
+    q.out = next, q.e = x.e + poly.e;
+    if (i + 1 < a.steps) product<kNext>(l, a.batch, operand(x), operand(poly), rk, q, parts, st);
+    else product<kLast>(l, a.batch, operand(x), operand(poly), rk, q, parts, st);
+    x = next;
   }
   return hipGetLastError();
 }

@@ -1,14 +1,15 @@
 """Linear cross entropy and its gradients: the library against the formulas in 64 bits.
 
-Tolerances, with u = 2^-24.  A logit is a sum of D products in fp32: exact products of pieces that
-hold 24 bits of each factor (what is dropped is below 8 u of a term), partial sums of at most
-|h_t| |w_v| and roundings that behave like a random walk, so it is off by e = u (8 + 2 sqrt(D)) max|h| max|w|
-(+ u |bias|).  lse is off by e, by 64 u relative of the sum of exponentials, and by u |lse|; a loss by
-twice that.  dl is off by (2 e + 64 u) |p| and 2 u |dl|; its products add u (8 + 2 sqrt(n)) of their magnitudes, n
-terms, and bf16 operands half a step, 2^-8, of every |dl| and once more of the result.  Below 2^-126
-fp32 and bf16 hold no full significand, and such values may count as zero: exp(l - lse), and each of the three
-pieces of dl, may lose 2^-126 that way, so a product's term 4 x 2^-126 times the other factor.  (Logits of hundreds
-have such probabilities, 1e-53 for instance, whose gradient in fp32 is zero and in 64 bits is not.)
+Tolerances, with u = 2^-24.  fp32 factors are held by two planes of fp16: to 2^-22 of themselves, values below
+2^-18 of the tensor's largest to 2^-40 of that (half of fp16's smallest step, 2^-25, under a power of two that
+brings the largest to 2^14 at least: 2^-39), and the product of two lower planes, below 2^-22 of the term, is left out: 12 u of a term.
+A logit is a sum of D such products in fp32: partial sums of at most |h_t| |w_v| and roundings that behave like
+a random walk, so it is off by e = u (12 + 2 sqrt(D)) max|h| max|w| (+ u |bias|).  lse is off by e, by 64 u relative
+of the sum of exponentials, and by u |lse|; a loss by twice that.  dl is off by (2 e + 64 u) |p| and 2 u |dl|; its
+products add u (12 + 2 sqrt(n)) of their magnitudes, n terms, with fp32 operands 2^-40 of the largest |dloss|
+(dl's planes hold it times 2^15 relative to that) times the other factor and 2^-39 of the other tensor's largest times dl;
+with bf16 operands half a step, 2^-8, of every |dl|; and a bf16 result half a step more.  Below 2^-126 fp32 and bf16
+hold no full significand, and such values may count as zero: 4 x 2^-126 times the other factor.
 """
 import numpy as np
 import pytest
@@ -73,7 +74,7 @@ def check(r, type, ignore_index=-100):
     bf = type == "bf16"
     b64 = None if b is None else b.astype(np.float64)
     loss, lse = tr.cross_entropy(h, w, b64, target, ignore_index)
-    e = U * (8 + 2 * np.sqrt(D)) * np.linalg.norm(h, axis=1).max() * np.linalg.norm(w, axis=1).max()
+    e = U * (12 + 2 * np.sqrt(D)) * np.linalg.norm(h, axis=1).max() * np.linalg.norm(w, axis=1).max()
     e += 0 if b is None else U * np.abs(b[np.isfinite(b)]).max(initial=0)
     with np.errstate(invalid="ignore"):
         tol = e + 64 * U + 2 * U * np.abs(lse)
@@ -90,7 +91,9 @@ def check(r, type, ignore_index=-100):
 
     def near(got, ref, a, m, n):
         # products of dl (with its error) and the other operand
-        tol = rounded_of(a) @ m + U * (8 + 2 * np.sqrt(n)) * (np.abs(a) @ m) + 2 * U * np.abs(ref)
+        tol = rounded_of(a) @ m + U * (12 + 2 * np.sqrt(n)) * (np.abs(a) @ m) + 2 * U * np.abs(ref)
+        if not bf:
+            tol += 2.0 ** -40 * np.abs(dloss[k]).max(initial=0) * m.sum(0) + 2.0 ** -39 * m.max(initial=0) * np.abs(a).sum(1, keepdims=True)
         tol += 2.0 ** -8 * np.abs(ref) if bf else 0
         tol += 4 * 2.0 ** -126 * (1 + np.abs(m).sum(0))
         assert (np.abs(got - ref) <= tol).all(), np.abs(got - ref).max()
