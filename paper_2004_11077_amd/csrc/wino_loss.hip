@@ -9,7 +9,7 @@
 // operand of the two products of the piece; h, W and dl enter those with k across their rows
 // (wino_products.hpp), so none of them is transposed in memory.
 //
-// bf16 operands are taken where they lie if their rows are whole blocks of 16 bytes and of 32 k, and
+// bf16 operands are taken where they lie if their rows are whole pieces of 16 bytes and whole lines, and
 // from a padded copy otherwise; dl is rounded to bf16 like the gradients.  fp32 operands become two
 // fp16 planes (22 bits) under one power of two for W and one for h (in the forward pass one a row, so that
 // no row's magnitude touches another's lse); in the backward pass rows that are left out count as
@@ -112,14 +112,13 @@ __global__ __launch_bounds__(256) void k_loss_range(const float* __restrict__ w,
   }
 }
 
-// One tensor to planes: [rows][cols] -> [rows][ld], columns from cols to ld zero.
+// One tensor to planes: [rows][cols] -> rows of ld elements, columns from cols to ld zero.
 struct Copy {
   const void* src;
   long src_ld;
   int rows, cols;
   uint16_t* dst;
   int ld;
-  long plane;
   int masked;             // rows that do not count as zeros
   const float* most;      // fp32: [kRange] partial maxima, null: one power of two a row, to `unit`
   float* unit;
@@ -153,7 +152,7 @@ __device__ __forceinline__ void copy_rows(const Copy& o, const Rows& g, unsigned
     }
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      *reinterpret_cast<uint4*>(o.dst + n * o.plane + r * o.ld + c) = *reinterpret_cast<const uint4*>(out[n]);
+      *reinterpret_cast<uint4*>(o.dst + r * o.ld * NP + place<NP>(c) + n * 32) = *reinterpret_cast<const uint4*>(out[n]);
   }
 }
 
@@ -178,7 +177,7 @@ __device__ __forceinline__ void copy_rows_apart(const Copy& o, unsigned block, u
       cut<2>(c + 1 < o.cols ? p[c + 1] * scale : 0.f, b);
 #pragma unroll
       for (int n = 0; n < 2; ++n)
-        *reinterpret_cast<ushort2*>(o.dst + n * o.plane + r * o.ld + c) = make_ushort2(a[n], b[n]);
+        *reinterpret_cast<ushort2*>(o.dst + r * o.ld * 2 + place<2>(c) + n * 32) = make_ushort2(a[n], b[n]);
     }
   }
 }
@@ -342,7 +341,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
                                                              int tiles_n, const float* __restrict__ lse,
                                                              const float* __restrict__ dloss,
                                                              const float* __restrict__ ref,
-                                                             uint16_t* __restrict__ dl, int ld, long plane,
+                                                             uint16_t* __restrict__ dl, int ld,
                                                              float* __restrict__ dbias) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
@@ -385,7 +384,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
       if (t < g.g.rows && v < ld) {   // ld is a multiple of 4; from the last class on d is zero
 #pragma unroll
         for (int p = 0; p < T::NP; ++p)
-          *reinterpret_cast<ushort4*>(dl + p * plane + (long)t * ld + v) =
+          *reinterpret_cast<ushort4*>(dl + (long)t * ld * T::NP + place<T::NP>(v) + p * 32) =
               make_ushort4(out[0][p], out[1][p], out[2][p], out[3][p]);
       }
     }
@@ -502,18 +501,19 @@ unsigned grid_of(long items, long most) {
   return (unsigned)(b < 1 ? 1 : b < most ? b : most);
 }
 
-// Tiles.  256 x 256 where they fill the chip, else 128 x 128, else 64 x 64.
+// Tiles.  256 x 256 where they fill the chip, else 128 x 128, else 64 x 64 (and two to five work
+// groups a compute unit).
 template <int NP, bool AX, bool BX>
 struct Tiles {
-  typedef Tile<256, 256, 2, 4, NP, NP == 1 ? 4 : 2, AX, BX> Big;
-  typedef Tile<128, 128, 2, NP == 1 ? 2 : 4, NP, 4, AX, BX> Mid;
-  typedef Tile<64, 64, 2, 2, NP, 4, AX, BX> Small;
+  typedef Tile<256, 256, 2, 4, NP, 2, AX, BX> Big;
+  typedef Tile<128, 128, 2, 2, NP, 2, AX, BX> Mid;
+  typedef Tile<64, 64, 2, 2, NP, 2, AX, BX> Small;
 };
 long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
 int side_for(long m, long n, long splits = 1) {
   return count_of(m, n, 256) * splits >= 160 ? 256 : count_of(m, n, 128) * splits >= 160 ? 128 : 64;
 }
-constexpr int waves_n(int side, int np) { return side == 256 ? 4 : side == 128 && np == 2 ? 4 : 2; }
+constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
 
 template <int NP, bool AX, bool BX, class F>
 void with_tile(int side, F&& f) {
@@ -522,9 +522,9 @@ void with_tile(int side, F&& f) {
   else f(typename Tiles<NP, AX, BX>::Small{});
 }
 
-// bf16 rows that the products can take where they lie: 16-byte accesses, whole blocks of k.
+// bf16 rows that the products can take where they lie: 16-byte accesses, whole stages of k.
 bool direct(const LossArgs& a, const void* p, long stride) {
-  return a.bf16 && a.features % 32 == 0 && stride % 8 == 0 && stride <= kMaxLd && ((uintptr_t)p & 15) == 0;
+  return a.bf16 && a.features % 64 == 0 && stride % 8 == 0 && stride <= kMaxLd && ((uintptr_t)p & 15) == 0;
 }
 
 const void* row_at(const LossArgs& a, const void* p, long row, long stride) {
@@ -538,16 +538,16 @@ void operands(const LossArgs& a, const LossLayout& l, const Rows& g, const void*
               hipStream_t st) {
   uint16_t* to_w = reinterpret_cast<uint16_t*>(ws + l.w);
   uint16_t* to_h = reinterpret_cast<uint16_t*>(ws + l.h);
-  const long pw = (long)count * l.dp, ph = (long)a.rows * l.dp;
-  const Copy cw{w_rows, a.w_stride, count, a.features, to_w, l.dp, pw, 0, num->max_w, &num->of_w};
-  const Copy ch{h, a.h_stride, a.rows, a.features, to_h, l.dp, ph, masked, h_apart ? nullptr : num->max_h,
+  const long pw = (long)count * l.dp / 8, ph = (long)a.rows * l.dp / 8;
+  const Copy cw{w_rows, a.w_stride, count, a.features, to_w, l.dp, 0, num->max_w, &num->of_w};
+  const Copy ch{h, a.h_stride, a.rows, a.features, to_h, l.dp, masked, h_apart ? nullptr : num->max_h,
                 h_apart ? reinterpret_cast<float*>(ws + l.unit) : &num->of_h};
-  const unsigned first = w_direct ? 0 : grid_of(pw / 8, 4096), more = h_ready ? 0 : grid_of(ph / 8, 4096);
+  const unsigned first = w_direct ? 0 : grid_of(pw, 4096), more = h_ready ? 0 : grid_of(ph, 4096);
   typedef typename std::conditional<NP == 1, uint16_t, float>::type T;
   if (first + more) wino_launch((k_loss_planes<T, NP>), dim3(first + more), dim3(256), st, cw, ch, first, g);
-  *ow = w_direct ? Operand{(const uint16_t*)w_rows, a.w_stride, 0, 0, count, a.features}
-                 : Operand{to_w, l.dp, pw, 0, count, l.dp};
-  if (!h_ready) *oh = Operand{to_h, l.dp, ph, 0, a.rows, l.dp};
+  *ow = w_direct ? Operand{(const uint16_t*)w_rows, a.w_stride, 0, count, a.features}
+                 : Operand{to_w, (long)l.dp * NP, 0, count, l.dp};
+  if (!h_ready) *oh = Operand{to_h, (long)l.dp * NP, 0, a.rows, l.dp};
 }
 
 template <int NP>
@@ -560,8 +560,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
   const Rows g{target, a.ignore_index, a.rows, a.classes};
   const bool w_direct = direct(a, w, a.w_stride);
   bool h_ready = direct(a, h, a.h_stride);
-  Operand oh{(const uint16_t*)h, a.h_stride, 0, 0, a.rows, a.features}, ow{};
-  const int k = NP == 1 && a.features % 32 == 0 ? a.features : l.dp;
+  Operand oh{(const uint16_t*)h, a.h_stride, 0, a.rows, a.features}, ow{};
   if (NP == 2)
     wino_launch(k_loss_range, dim3(kRange), dim3(256), st, (const float*)w, a.w_stride, (const float*)nullptr, 0L,
                 a.features, g, (const float*)nullptr, num);
@@ -569,7 +568,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
   const long most = (1L << 21) / ((a.rows + 63) / 64) * 64;
   long piece = w_direct ? a.classes : l.piece;
   if (piece > most) piece = most < 256 ? 256 : most / 256 * 256;
-  Logits q{bias, g, 0, 0, k, &num->of_w, reinterpret_cast<const float*>(ws + l.unit), 1};
+  Logits q{bias, g, 0, 0, l.dp, &num->of_w, reinterpret_cast<const float*>(ws + l.unit), 1};
   int part = 0;
   for (long first = 0; first < a.classes; first += piece) {
     q.first = (int)first;
@@ -607,7 +606,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
   const bool w_direct = direct(a, w, a.w_stride);
   bool h_ready = false;   // always a copy: rows that are left out as zeros
   Operand oh{}, ow{};
-  Logits q{bias, g, 0, 0, NP == 1 && a.features % 32 == 0 ? a.features : l.dp, &num->of_w, &num->of_h, 0};
+  Logits q{bias, g, 0, 0, l.dp, &num->of_w, &num->of_h, 0};
   uint16_t* dl = reinterpret_cast<uint16_t*>(ws + l.dl);
   float* db = dbias ? reinterpret_cast<float*>(ws + l.dbias) : nullptr;
   float* sums = reinterpret_cast<float*>(ws + l.dh);
@@ -620,15 +619,14 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
     operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, true, num, ws, &ow, &oh,
                  st);
     h_ready = true;
-    const long plane = (long)a.rows * vp;
     with_tile<NP, false, false>(l.side, [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
       parts = tn * T::WN;
       wino_launch((k_loss_dlogits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, lse, dloss, ref, dl, vp,
-                  plane, db);
+                  db);
     });
-    const Operand od{dl, vp, plane, 0, a.rows, vp};
+    const Operand od{dl, (long)vp * NP, 0, a.rows, vp};
     if (dh) {
       const int per = (int)up((vp + l.splits - 1) / l.splits, 64);
       Product p{one ? dh : (void*)sums, a.features, (long)a.rows * a.features, one ? a.bf16 : first ? 3 : 2, vp, per,
@@ -640,7 +638,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
       });
     }
     if (dw) {
-      const int tk = (int)up(a.rows, 32);
+      const int tk = (int)up(a.rows, 64);
       Product p{const_cast<void*>(row_at(a, dw, first, a.features)), a.features, 0, a.bf16, tk, tk, a.features, q.count,
                 ref, &num->of_h};
       with_tile<NP, true, true>(side_for(a.features, q.count), [&](auto tile) {
@@ -666,11 +664,12 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
   const int np = a.bf16 ? 1 : 2;
   const size_t item = 2 * (size_t)np;   // bytes of a value in planes
   l.dp = (int)up(D, 64);
-  // classes per piece: what the caller asks for, or as many as keep a piece's dl and planes of W within
-  // 256 MiB
-  size_t piece = a.piece ? (size_t)a.piece : ((size_t)256 << 20) / (item * (T + l.dp));
+  // classes per piece: what the caller asks for, or as many as keep a piece's dl, and its planes of W,
+  // within 256 MiB
+  const size_t most = T > (size_t)l.dp ? T : (size_t)l.dp;
+  size_t piece = a.piece ? (size_t)a.piece : ((size_t)256 << 20) / (item * most);
   piece = up(piece < 1024 && !a.piece ? 1024 : piece, 256);
-  if (piece > (size_t)kMaxLd) piece = (size_t)kMaxLd;
+  if (piece > (size_t)kMaxLd / 2) piece = (size_t)kMaxLd / 2;   // rows of dl on two planes
   l.piece = (int)(piece < V ? piece : V);
   const size_t P = (size_t)l.piece, vp = up(P, 64);
   size_t at = 0;
@@ -696,7 +695,7 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
     if (s > room) s = room;
     l.splits = (int)(s < 1 ? 1 : s);
     l.dh = take(4 * T * D * l.splits);
-    l.dbias = take(4 * V * waves_n(l.side, np) * (T ? (T + l.side - 1) / l.side : 1));
+    l.dbias = take(4 * V * waves_n(l.side) * (T ? (T + l.side - 1) / l.side : 1));
   }
   l.bytes = at;
   return l;

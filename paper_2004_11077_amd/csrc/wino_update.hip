@@ -56,32 +56,35 @@ __global__ __launch_bounds__(256) void k_update_norm(const void* __restrict__ g,
 // values.
 struct Planes {
   uint16_t* p;
-  long plane, batch;
+  long batch;
   int ld, e;
+  __device__ __forceinline__ uint16_t* at(int row, int k) const {
+    return p + blockIdx.z * batch + (long)row * ld * 2 + place<2>(k);
+  }
 };
 
 // Four consecutive elements of a row, from a multiple of four.
 __device__ __forceinline__ void put(const Planes& o, int row, int k, f32x4 v) {
-  uint16_t* to = o.p + blockIdx.z * o.batch + (long)row * o.ld + k;
+  uint16_t* to = o.at(row, k);
   const float s = power(o.e);
   uint16_t q[4][2];
 #pragma unroll
   for (int e = 0; e < 4; ++e) cut<2>(v[e] * s, q[e]);
 #pragma unroll
   for (int p = 0; p < 2; ++p)
-    *reinterpret_cast<ushort4*>(to + p * o.plane) = make_ushort4(q[0][p], q[1][p], q[2][p], q[3][p]);
+    *reinterpret_cast<ushort4*>(to + p * 32) = make_ushort4(q[0][p], q[1][p], q[2][p], q[3][p]);
 }
 // The same four values as one element of four consecutive rows.
 __device__ __forceinline__ void put_across(const Planes& o, int row, int k, int rows, f32x4 v) {
-  uint16_t* to = o.p + blockIdx.z * o.batch + (long)row * o.ld + k;
+  uint16_t* to = o.at(row, k);
   const float s = power(o.e);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if (row + e >= rows) continue;
     uint16_t q[2];
     cut<2>(v[e] * s, q);
-    to[(long)e * o.ld] = q[0];
-    to[o.plane + (long)e * o.ld] = q[1];
+    to[(long)e * o.ld * 2] = q[0];
+    to[(long)e * o.ld * 2 + 32] = q[1];
   }
 }
 
@@ -124,9 +127,9 @@ __global__ __launch_bounds__(256) void k_update_planes(const void* __restrict__ 
       out[0][e] = h[0];
       out[1][e] = h[1];
     }
-    uint16_t* to = x.p + blockIdx.z * x.batch + (long)(r0 + row) * x.ld + c0 + k;
+    uint16_t* to = x.at(r0 + row, c0 + k);
     *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(out[0]);
-    *reinterpret_cast<uint4*>(to + x.plane) = *reinterpret_cast<const uint4*>(out[1]);
+    *reinterpret_cast<uint4*>(to + 32) = *reinterpret_cast<const uint4*>(out[1]);
   }
 }
 
@@ -154,8 +157,8 @@ __device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, b
   const int km = KIND <= kPoly ? s.r : s.c;   // rows of the first operand
   if constexpr (KIND == kPoly) {
     if (n < s.r && m < s.gram.ld) {
-      const uint16_t* at = s.gram.p + blockIdx.z * s.gram.batch + (long)n * s.gram.ld + m;
-      const ushort4 h = *reinterpret_cast<const ushort4*>(at), l = *reinterpret_cast<const ushort4*>(at + s.gram.plane);
+      const uint16_t* at = s.gram.at(n, m);
+      const ushort4 h = *reinterpret_cast<const ushort4*>(at), l = *reinterpret_cast<const ushort4*>(at + 32);
       const float one = power(-s.gram.e);
       const float old[4] = {f16_value(h.x) + f16_value(l.x), f16_value(h.y) + f16_value(l.y),
                             f16_value(h.z) + f16_value(l.z), f16_value(h.w) + f16_value(l.w)};
@@ -251,13 +254,9 @@ __global__ __launch_bounds__(256) void k_update_few(Operand x, Operand y, int k,
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m0 = blockIdx.x % tiles_m * 32, n0 = blockIdx.x / tiles_m * 32;
-  __amdgpu_buffer_rsrc_t rx[2], ry[2];
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int left_x = x.rows - m0 < 32 ? x.rows - m0 : 32, left_y = y.rows - n0 < 32 ? y.rows - n0 : 32;
-    rx[q] = window(x.p + q * x.plane + blockIdx.z * x.batch + (long)m0 * x.ld, left_x * x.ld * 2);
-    ry[q] = window(y.p + q * y.plane + blockIdx.z * y.batch + (long)n0 * y.ld, left_y * y.ld * 2);
-  }
+  const int left_x = x.rows - m0 < 32 ? x.rows - m0 : 32, left_y = y.rows - n0 < 32 ? y.rows - n0 : 32;
+  const auto rx = window(x.p + blockIdx.z * x.batch + (long)m0 * x.ld, left_x * x.ld * 2);
+  const auto ry = window(y.p + blockIdx.z * y.batch + (long)n0 * y.ld, left_y * y.ld * 2);
   const int ax = ((lane & 15) * (int)x.ld + (lane >> 4) * 8) * 2, ay = ((lane & 15) * (int)y.ld + (lane >> 4) * 8) * 2;
   const int at_x[2] = {ax, ax + 32 * (int)x.ld}, at_y[2] = {ay, ay + 32 * (int)y.ld};
   f32x4 acc[2][2] = {};
@@ -267,13 +266,13 @@ __global__ __launch_bounds__(256) void k_update_few(Operand x, Operand y, int k,
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
       // beyond the last block: any block, and not multiplied
-      const int to = (b + d * 4 < blocks ? b + d * 4 : b) * 64;
+      const int to = (b + d * 4 < blocks ? b + d * 4 : b) * 128;
 #pragma unroll
       for (int q = 0; q < 2; ++q)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          fx[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx[q], at_x[i], to, 0));
-          fy[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry[q], at_y[i], to, 0));
+          fx[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, at_x[i] + q * 64, to, 0));
+          fy[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry, at_y[i] + q * 64, to, 0));
         }
     }
     __builtin_amdgcn_sched_barrier(0);   // all loads first
@@ -308,8 +307,8 @@ __global__ __launch_bounds__(256) void k_update_few(Operand x, Operand y, int k,
 template <bool AX>
 struct Tiles {
   typedef Tile<256, 256, 2, 4, 2, 2, AX> Big;
-  typedef Tile<128, 128, 2, 4, 2, 4, AX> Mid;
-  typedef Tile<64, 64, 2, 2, 2, 4, AX> Small;
+  typedef Tile<128, 128, 2, 2, 2, 2, AX> Mid;
+  typedef Tile<64, 64, 2, 2, 2, 2, AX> Small;
 };
 
 int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
@@ -394,10 +393,10 @@ hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, 
   double* norms = reinterpret_cast<double*>(ws + l.norms);
   wino_launch(k_update_norm, dim3(kNormParts, a.batch), dim3(256), st, g, a, norms);
   const auto planes = [&](size_t at, int ld, int e) {
-    const long items = (long)l.r * ld;
-    return Planes{reinterpret_cast<uint16_t*>(ws + at), items * a.batch, items, ld, e};
+    const long items = (long)l.r * ld * 2;
+    return Planes{reinterpret_cast<uint16_t*>(ws + at), items, ld, e};
   };
-  const auto operand = [&](const Planes& p) { return Operand{p.p, p.ld, p.plane, p.batch, l.r, p.ld}; };
+  const auto operand = [&](const Planes& p) { return Operand{p.p, p.ld * 2L, p.batch, l.r, p.ld}; };
   // largest singular value that X can have
   double s = 1;
   Planes x = planes(l.x, l.cp, exponent(s));
