@@ -120,7 +120,7 @@ struct Copy {
   uint16_t* dst;
   int ld;
   int masked;             // rows that do not count as zeros
-  const float* most;      // fp32: [kRange] partial maxima, null: one power of two a row, to `unit`
+  const float* most;      // fp32: [kRange] partial maxima; null: one power of two a row, to `unit`
   float* unit;
 };
 
@@ -186,9 +186,11 @@ __device__ __forceinline__ void copy_rows_apart(const Copy& o, unsigned block, u
 template <class T, int NP>
 __global__ __launch_bounds__(256) void k_loss_planes(Copy w, Copy h, unsigned first, Rows g) {
   __shared__ float lds[4];
-  if (blockIdx.x < first) copy_rows<T, NP>(w, g, blockIdx.x, first, lds);
-  else if (NP == 2 && !h.most) copy_rows_apart(h, blockIdx.x - first, gridDim.x - first);
-  else copy_rows<T, NP>(h, g, blockIdx.x - first, gridDim.x - first, lds);
+  const bool of_w = blockIdx.x < first;
+  const Copy& o = of_w ? w : h;
+  const unsigned block = of_w ? blockIdx.x : blockIdx.x - first, blocks = of_w ? first : gridDim.x - first;
+  if (NP == 2 && !o.most) copy_rows_apart(o, block, blocks);
+  else copy_rows<T, NP>(o, g, block, blocks, lds);
 }
 
 // What the logits of a piece need besides the operands.
@@ -197,9 +199,9 @@ struct Logits {
   Rows g;
   int first, count;          // classes of this piece
   int k;                     // features in whole blocks
-  const float* of_w;         // fp32: the planes' units; of h one for all rows or one a row
+  const float* of_w;         // fp32: the planes' units, one for all rows or (apart) one a row
   const float* of_h;
-  int h_apart;
+  int apart;
 };
 
 // Work group of the grid -> tile (m, n).  Consecutive work groups go round robin over the 8 XCDs: each
@@ -218,11 +220,14 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& m,
 template <class T>
 __device__ __forceinline__ void to_logits(const Logits& g, int v0, int j_t, f32x4 (&acc)[T::TM][T::TN], int j) {
   if constexpr (T::NP == 2) {
-    const float u = *g.of_w * g.of_h[g.h_apart ? j_t : 0];
+    const float u = g.of_h[g.apart ? j_t : 0];
 #pragma unroll
     for (int i = 0; i < T::TM; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][j][e] *= u;
+      for (int e = 0; e < 4; ++e) {
+        const int v = v0 + i * 16 + e;
+        acc[i][j][e] *= g.of_w[!g.apart ? 0 : v < g.count ? v : g.count - 1] * u;
+      }
   }
   if (g.bias || v0 + T::TM * 16 > g.count) {
 #pragma unroll
@@ -386,6 +391,11 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
         for (int p = 0; p < T::NP; ++p)
           *reinterpret_cast<ushort4*>(dl + (long)t * ld * T::NP + place<T::NP>(v) + p * 32) =
               make_ushort4(out[0][p], out[1][p], out[2][p], out[3][p]);
+        // tiles of 32 end where the line's last ones have no rows of W: zeros behind them
+        if (is_few<T> && tm + 1 == tiles_m && v + 32 < ld)
+#pragma unroll
+          for (int p = 0; p < T::NP; ++p)
+            *reinterpret_cast<ushort4*>(dl + (long)t * ld * T::NP + place<T::NP>(v + 32) + p * 32) = make_ushort4(0, 0, 0, 0);
       }
     }
   }
@@ -511,13 +521,20 @@ struct Tiles {
 };
 long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
 int side_for(long m, long n, long splits = 1) {
-  return count_of(m, n, 256) * splits >= 160 ? 256 : count_of(m, n, 128) * splits >= 160 ? 128 : 64;
+  return count_of(m, n, 256) * splits >= 512 ? 256 : count_of(m, n, 128) * splits >= 256 ? 128 : 64;
+}
+// The same of products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the
+// waves where there are few tiles.
+int side_along(long m, long n, long k) {
+  const int side = side_for(m, n);
+  return side == 64 && count_of(m, n, 64) < 64 && k >= 256 ? 32 : side;
 }
 constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
 
 template <int NP, bool AX, bool BX, class F>
 void with_tile(int side, F&& f) {
   if (side == 256) f(typename Tiles<NP, AX, BX>::Big{});
+  else if (side == 32 && !AX && !BX) f(Few<NP>{});
   else if (side == 128) f(typename Tiles<NP, AX, BX>::Mid{});
   else f(typename Tiles<NP, AX, BX>::Small{});
 }
@@ -534,15 +551,18 @@ const void* row_at(const LossArgs& a, const void* p, long row, long stride) {
 // Operands of a piece: where they lie, or planes made here.
 template <int NP>
 void operands(const LossArgs& a, const LossLayout& l, const Rows& g, const void* w_rows, int count, const void* h,
-              bool w_direct, bool h_ready, bool h_apart, bool masked, Numbers* num, char* ws, Operand* ow, Operand* oh,
+              bool w_direct, bool h_ready, bool back, Numbers* num, char* ws, Operand* ow, Operand* oh,
               hipStream_t st) {
   uint16_t* to_w = reinterpret_cast<uint16_t*>(ws + l.w);
   uint16_t* to_h = reinterpret_cast<uint16_t*>(ws + l.h);
   const long pw = (long)count * l.dp / 8, ph = (long)a.rows * l.dp / 8;
-  const Copy cw{w_rows, a.w_stride, count, a.features, to_w, l.dp, 0, num->max_w, &num->of_w};
-  const Copy ch{h, a.h_stride, a.rows, a.features, to_h, l.dp, masked, h_apart ? nullptr : num->max_h,
-                h_apart ? reinterpret_cast<float*>(ws + l.unit) : &num->of_h};
-  const unsigned first = w_direct ? 0 : grid_of(pw, 4096), more = h_ready ? 0 : grid_of(ph, 4096);
+  const Copy cw{w_rows, a.w_stride, count, a.features, to_w, l.dp, 0, back ? num->max_w : nullptr,
+                back ? &num->of_w : reinterpret_cast<float*>(ws + l.unit_w)};
+  const Copy ch{h, a.h_stride, a.rows, a.features, to_h, l.dp, back, back ? num->max_h : nullptr,
+                back ? &num->of_h : reinterpret_cast<float*>(ws + l.unit_h)};
+  // a wave a row, or a thread eight values
+  const auto grid = [&](long rows, long eights) { return NP == 2 && !back ? grid_of(rows * 64, 2048) : grid_of(eights, 2048); };
+  const unsigned first = w_direct ? 0 : grid(count, pw), more = h_ready ? 0 : grid(a.rows, ph);
   typedef typename std::conditional<NP == 1, uint16_t, float>::type T;
   if (first + more) wino_launch((k_loss_planes<T, NP>), dim3(first + more), dim3(256), st, cw, ch, first, g);
   *ow = w_direct ? Operand{(const uint16_t*)w_rows, a.w_stride, 0, count, a.features}
@@ -561,22 +581,18 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
   const bool w_direct = direct(a, w, a.w_stride);
   bool h_ready = direct(a, h, a.h_stride);
   Operand oh{(const uint16_t*)h, a.h_stride, 0, a.rows, a.features}, ow{};
-  if (NP == 2)
-    wino_launch(k_loss_range, dim3(kRange), dim3(256), st, (const float*)w, a.w_stride, (const float*)nullptr, 0L,
-                a.features, g, (const float*)nullptr, num);
   // a launch holds fewer than 2^32 threads
   const long most = (1L << 21) / ((a.rows + 63) / 64) * 64;
   long piece = w_direct ? a.classes : l.piece;
   if (piece > most) piece = most < 256 ? 256 : most / 256 * 256;
-  Logits q{bias, g, 0, 0, l.dp, &num->of_w, reinterpret_cast<const float*>(ws + l.unit), 1};
+  Logits q{bias, g, 0, 0, l.dp, reinterpret_cast<const float*>(ws + l.unit_w), reinterpret_cast<const float*>(ws + l.unit_h), 1};
   int part = 0;
   for (long first = 0; first < a.classes; first += piece) {
     q.first = (int)first;
     q.count = (int)(a.classes - first < piece ? a.classes - first : piece);
-    operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, NP == 2, false, num, ws, &ow,
-                 &oh, st);
+    operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, num, ws, &ow, &oh, st);
     h_ready = true;
-    with_tile<NP, false, false>(side_for(q.count, a.rows), [&](auto tile) {
+    with_tile<NP, false, false>(side_along(q.count, a.rows, l.dp), [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
       wino_launch((k_loss_logits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, part, best, hit);
@@ -616,8 +632,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
     q.first = (int)first;
     q.count = a.classes - q.first < l.piece ? a.classes - q.first : l.piece;
     const int vp = (int)up(q.count, 64);
-    operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, true, num, ws, &ow, &oh,
-                 st);
+    operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, true, num, ws, &ow, &oh, st);
     h_ready = true;
     with_tile<NP, false, false>(l.side, [&](auto tile) {
       typedef decltype(tile) T;
@@ -680,18 +695,20 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
   l.splits = 1;
   if (!back) {
     // pieces are whole multiples of 256 classes, so no tile spans two
-    const size_t least = T >= 160 * 256 ? 256 : T >= 160 * 128 ? 128 : 64;   // of side_for() for any classes
+    const size_t least = T >= 512 * 256 ? 256 : T >= 256 * 128 ? 128 : T >= 64 * 64 ? 64 : 32;   // of side_along() for any classes
     l.parts = take(8 * T * (up(V, 256) / least));
     l.target = take(4 * T);
-    l.unit = take(4 * T);
+    l.unit_w = take(4 * P);
+    l.unit_h = take(4 * T);
   } else {
     l.dl = take(item * T * vp);
-    l.side = side_for((long)P, (long)T);
+    l.side = side_along((long)P, (long)T, l.dp);
     // ranges of classes until dh's tiles fill the chip, each of 512 classes or more
     const long room = (long)(vp / 512 ? vp / 512 : 1);
-    l.dh_side = side_for((long)D, (long)T, room < 8 ? room : 8);
+    l.dh_side = count_of((long)D, (long)T, 256) >= 100 ? 256 : side_for((long)D, (long)T, room < 8 ? room : 8);
     const long tiles = T ? count_of((long)D, (long)T, l.dh_side) : 1;
-    long s = (256 + tiles - 1) / tiles;
+    const long full = l.dh_side == 256 ? 256 : 512;
+    long s = (full + tiles - 1) / tiles;
     if (s > room) s = room;
     l.splits = (int)(s < 1 ? 1 : s);
     l.dh = take(4 * T * D * l.splits);

@@ -102,6 +102,20 @@ struct Tile {
   static_assert(COPIES * (RING - 2) < 64);   // what a counted wait can say
 };
 
+// Products of few tiles and k along the rows of both operands, where waiting counts: 32 x 32 of D a
+// work group.  Its WAVES waves take every WAVES-th line of k, fragments straight from memory into
+// registers, many lines under way and no barrier in the loop; their sums are joined in LDS, after which
+// each of the first four waves has one of the four 16 x 16 blocks, as if the tile were 2 x 2 waves.
+template <int NP_, int WAVES_ = 4>
+struct Few {
+  static constexpr int BM = 32, BN = 32, WM = 2, WN = 2, NP = NP_, WAVES = WAVES_, TM = 1, TN = 1;
+  static constexpr int THREADS = 64 * WAVES, K = 64 / NP, LDS = WAVES * 4096;
+};
+template <class T>
+constexpr bool is_few = false;
+template <int NP, int WAVES>
+constexpr bool is_few<Few<NP, WAVES>> = true;
+
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const uint16_t* p, long bytes) {
   const int size = bytes < 0 ? 0 : bytes > 0x7fffffff ? 0x7fffffff : (int)bytes;
@@ -195,12 +209,75 @@ struct Side {
 };
 #endif
 
+#if defined(__HIP_DEVICE_COMPILE__)
+// Two planes: upper and lower, lower and upper, upper and upper; one: its two parts of 32 k each.
+template <int NP, int TM, int TN>
+__device__ __forceinline__ void multiply_parts(const u32x4 (&a)[2][TM], const u32x4 (&b)[2][TN], f32x4 (&acc)[TM][TN]) {
+#pragma unroll
+  for (int s = 0; s < (NP == 1 ? 2 : 3); ++s) {
+    const int p = NP == 1 ? s : s == 1, q = NP == 1 ? s : s == 0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = multiply_block<NP>(a[p][i], b[q][j], acc[i][j]);
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void multiply_few(const Operand& a, const Operand& b, long batch, int m0, int n0,
+                                             int k_begin, int k_end, char* lds, f32x4& out) {
+  constexpr int DEPTH = 4;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int left_a = a.rows - m0 < 32 ? a.rows - m0 : 32, left_b = b.rows - n0 < 32 ? b.rows - n0 : 32;
+  const auto ra = window(a.p + batch * a.batch + (long)m0 * a.ld, ((left_a - 1) * a.ld + (long)a.cols * T::NP) * 2);
+  const auto rb = window(b.p + batch * b.batch + (long)n0 * b.ld, ((left_b - 1) * b.ld + (long)b.cols * T::NP) * 2);
+  const int at_a = ((lane & 15) * (int)a.ld + (lane >> 4) * 8) * 2, at_b = ((lane & 15) * (int)b.ld + (lane >> 4) * 8) * 2;
+  const int next_a = 32 * (int)a.ld, next_b = 32 * (int)b.ld;   // 16 rows on, bytes
+  f32x4 acc[2][2] = {};
+  const int lines = k_end / T::K;
+  for (int l = k_begin / T::K + wave; l < lines; l += DEPTH * T::WAVES) {
+    u32x4 fa[DEPTH][2][2], fb[DEPTH][2][2];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      // lines beyond the last one: out of the window, zeros
+      const int line = l + d * T::WAVES, off = line < lines ? 0 : 0x40000000;
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int to = off ? 0 : line * 128;
+          fa[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, (at_a + i * next_a + q * 64) | off, to, 0));
+          fb[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rb, (at_b + i * next_b + q * 64) | off, to, 0));
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);   // all loads before the first product
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) multiply_parts<T::NP>(fa[d], fb[d], acc);
+  }
+  f32x4* join = reinterpret_cast<f32x4*>(lds);   // [wave][block][lane]
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) join[(wave * 4 + j * 2 + i) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  if (wave < 4) {   // block (wave % 2, wave / 2)
+    out = join[wave * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < T::WAVES; ++w) out += join[(w * 4 + wave) * 64 + lane];
+  }
+}
+#endif
+
 // acc[i][j] += blocks of D for m0 .. and n0 .., k from k_begin to k_end (multiples of T::K).  lds: T::LDS
 // bytes.
 template <class T>
 __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, long batch, int m0, int n0,
                                          int k_begin, int k_end, char* lds, f32x4 (&acc)[T::TM][T::TN]) {
 #if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (is_few<T>) {
+    multiply_few<T>(a, b, batch, m0, n0, k_begin, k_end, lds, acc[0][0]);
+  } else {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
@@ -222,15 +299,7 @@ __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, lon
       for (int j = 0; j < T::TN; ++j) fb[q][j] = sb.fragment(from + B_AT, q, wn * T::TN + j);
     }
     __builtin_amdgcn_s_setprio(1);
-    // two planes: upper and lower, lower and upper, upper and upper; one: its 32 k each
-#pragma unroll
-    for (int s = 0; s < (T::NP == 1 ? 2 : 3); ++s) {
-      const int p = T::NP == 1 ? s : s == 1, q = T::NP == 1 ? s : s == 0;
-#pragma unroll
-      for (int i = 0; i < T::TM; ++i)
-#pragma unroll
-        for (int j = 0; j < T::TN; ++j) acc[i][j] = multiply_block<T::NP>(fa[p][i], fb[q][j], acc[i][j]);
-    }
+    multiply_parts<T::NP>(fa, fb, acc);
     __builtin_amdgcn_s_setprio(0);
   };
   const int stages = (k_end - k_begin) / T::K;
@@ -250,6 +319,7 @@ __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, lon
     work(lds + slot * T::STAGE);
     slot = slot + 1 == T::RING ? 0 : slot + 1;
     next = next + 1 == T::RING ? 0 : next + 1;
+  }
   }
 #endif
 }

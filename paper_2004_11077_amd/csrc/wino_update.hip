@@ -244,63 +244,17 @@ __global__ __launch_bounds__(256) void k_update_join(const float* __restrict__ p
   }
 }
 
-// Products of few tiles and k along the rows of both operands, where waiting counts: 32 x 32 of D a
-// work group, whose four waves take every fourth block of k, fragments straight from memory into
-// registers, no barrier in the loop; their sums are joined in LDS.
-template <Kind KIND>
-__global__ __launch_bounds__(256) void k_update_few(Operand x, Operand y, int k, int tiles_m, Result s) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int DEPTH = 4;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m0 = blockIdx.x % tiles_m * 32, n0 = blockIdx.x / tiles_m * 32;
-  const int left_x = x.rows - m0 < 32 ? x.rows - m0 : 32, left_y = y.rows - n0 < 32 ? y.rows - n0 : 32;
-  const auto rx = window(x.p + blockIdx.z * x.batch + (long)m0 * x.ld, left_x * x.ld * 2);
-  const auto ry = window(y.p + blockIdx.z * y.batch + (long)n0 * y.ld, left_y * y.ld * 2);
-  const int ax = ((lane & 15) * (int)x.ld + (lane >> 4) * 8) * 2, ay = ((lane & 15) * (int)y.ld + (lane >> 4) * 8) * 2;
-  const int at_x[2] = {ax, ax + 32 * (int)x.ld}, at_y[2] = {ay, ay + 32 * (int)y.ld};
-  f32x4 acc[2][2] = {};
-  const int blocks = k / 32;
-  for (int b = wave; b < blocks; b += DEPTH * 4) {
-    u32x4 fx[DEPTH][2][2], fy[DEPTH][2][2];
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      // beyond the last block: any block, and not multiplied
-      const int to = (b + d * 4 < blocks ? b + d * 4 : b) * 128;
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          fx[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, at_x[i] + q * 64, to, 0));
-          fy[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry, at_y[i] + q * 64, to, 0));
-        }
-    }
-    __builtin_amdgcn_sched_barrier(0);   // all loads first
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      if (b + d * 4 >= blocks) break;
-#pragma unroll
-      for (int t = 1; t >= 0; --t)
-#pragma unroll
-        for (int q = 0; q <= t; ++q)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = multiply_block<2>(fx[d][q][i], fy[d][t - q][j], acc[i][j]);
-    }
-  }
-  __shared__ f32x4 join[4][4][64];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) join[wave][i * 2 + j][lane] = acc[i][j];
-  __syncthreads();
-  // one of the four 16 x 16 blocks a wave
-  f32x4 v = join[0][wave][lane];
-#pragma unroll
-  for (int w = 1; w < 4; ++w) v += join[w][wave][lane];
-  finish<KIND>(s, m0 + (wave >> 1) * 16 + (lane >> 4) * 4, n0 + (wave & 1) * 16 + (lane & 15), v, false);
-#endif
+// The symmetric products of few rows.
+template <Kind KIND, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_update_few(Operand x, int k, int tiles, Result s) {
+  typedef Few<2, WAVES> T;
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+  const int m0 = blockIdx.x % tiles * 32, n0 = blockIdx.x / tiles * 32;
+  f32x4 acc[1][1] = {};
+  multiply<T>(x, x, blockIdx.z, m0, n0, 0, k, lds, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (wave >= 4) return;
+  finish<KIND>(s, m0 + (wave & 1) * 16 + (lane >> 4) * 4, n0 + (wave >> 1) * 16 + (lane & 15), acc[0][0], false);
 }
 
 // Tiles of products; AX: k across the rows of the first operand (X in P X).
@@ -322,19 +276,26 @@ void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& 
              float* parts, hipStream_t st) {
   if constexpr (KIND <= kPoly) {
     if (few(l, batch)) {
+      // eight waves where four would have more than four lines of k each
       const int tm = tiles_of(l.r, 32);
-      wino_launch((k_update_few<KIND>), dim3(tm * tm, 1, batch), dim3(256), st, x, y, k, tm, s);
+      const dim3 grid(tm * tm, 1, batch);
+      if (k > 32 * 4 * 4) wino_launch((k_update_few<KIND, 8>), grid, dim3(512), st, x, k, tm, s);
+      else wino_launch((k_update_few<KIND, 4>), grid, dim3(256), st, x, k, tm, s);
       return;
     }
-    typedef Tiles<false>::Mid T;
-    const int tm = tiles_of(l.r, T::BM), splits = KIND == kGram ? l.splits : 1;
-    const int per = (int)up((k + splits - 1) / splits, 32);
-    const long part = (long)batch * l.r * l.rp;
-    wino_launch((k_update_product<T, KIND>), dim3(half_of(tm), splits, batch), dim3(T::THREADS), st, x, y, k, per, tm, s,
-                splits > 1 ? parts : nullptr, part, l.rp);
-    if (splits > 1)
-      wino_launch((k_update_join<KIND>), dim3(half_of(tiles_of(l.rp, 64)), 1, batch), dim3(256), st,
-                  (const float*)parts, splits, part, l.rp, s);
+    const auto go = [&](auto tile) {
+      typedef decltype(tile) T;
+      const int tm = tiles_of(l.r, T::BM), splits = KIND == kGram ? l.splits : 1;
+      const int per = (int)up((k + splits - 1) / splits, 32);
+      const long part = (long)batch * l.r * l.rp;
+      wino_launch((k_update_product<T, KIND>), dim3(half_of(tm), splits, batch), dim3(T::THREADS), st, x, y, k, per, tm,
+                  s, splits > 1 ? parts : nullptr, part, l.rp);
+      if (splits > 1)
+        wino_launch((k_update_join<KIND>), dim3(half_of(tiles_of(l.rp, 64)), 1, batch), dim3(256), st,
+                    (const float*)parts, splits, part, l.rp, s);
+    };
+    if (half_of(tiles_of(l.r, 128)) * batch >= 512) go(Tiles<false>::Mid{});
+    else go(Tiles<false>::Small{});
   } else {
     const auto go = [&](auto tile) {
       typedef decltype(tile) T;
@@ -343,8 +304,8 @@ void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& 
                   (float*)nullptr, 0L, 0);
     };
     const auto count = [&](int side) { return (long)tiles_of(l.c, side) * tiles_of(l.r, side) * batch; };
-    if (count(256) >= 128) go(Tiles<true>::Big{});
-    else if (count(128) >= 128) go(Tiles<true>::Mid{});
+    if (count(256) >= 512) go(Tiles<true>::Big{});
+    else if (count(128) >= 192) go(Tiles<true>::Mid{});
     else go(Tiles<true>::Small{});
   }
 }
@@ -376,10 +337,10 @@ UpdateLayout update_layout(const UpdateArgs& a) {
   l.poly = take(item * l.r * l.rp);
   l.splits = 1;
   if (a.batch && l.r && !few(l, a.batch)) {
-    // ranges of A's k until its tiles fill the chip, each of 256 or more
-    const long tiles = (long)half_of(tiles_of(l.r, 128)) * a.batch;
-    long s = (256 + tiles - 1) / tiles;
-    if (s > l.cp / 256) s = l.cp / 256;
+    // ranges of A's k until its tiles of 64 x 64 fill the chip, each of 512 or more
+    const long tiles = (long)half_of(tiles_of(l.r, 64)) * a.batch;
+    long s = 512 / tiles;
+    if (s > l.cp / 512) s = l.cp / 512;
     l.splits = (int)(s < 1 ? 1 : s);
     if (l.splits > 1) l.parts = take(4 * (size_t)l.splits * a.batch * l.r * l.rp);
   }
