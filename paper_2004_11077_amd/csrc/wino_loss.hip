@@ -204,18 +204,6 @@ struct Logits {
   int apart;
 };
 
-// Work group of the grid -> tile (m, n).  Consecutive work groups go round robin over the 8 XCDs: each
-// XCD takes a run of tiles, in which bands of eight tiles m keep their rows in its L2 while those of n
-// pass.
-__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& m, int& n) {
-  const int all = tiles_m * tiles_n, per = all / 8;
-  if (b < per * 8) b = (b & 7) * per + (b >> 3);
-  const int band = b / (8 * tiles_n), rest = b - band * 8 * tiles_n;
-  const int wide = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
-  m = band * 8 + rest % wide;
-  n = rest / wide;
-}
-
 // Products -> logits of a tile: units, bias, and -infinity beyond the last class.
 template <class T>
 __device__ __forceinline__ void to_logits(const Logits& g, int v0, int j_t, f32x4 (&acc)[T::TM][T::TN], int j) {
@@ -249,7 +237,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_logits(Operand w, Operand h
                                                             float* __restrict__ hit) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
-  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  tile_at(place_of_group(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
   multiply<T>(w, h, 0, m0, n0, 0, g.k, lds, acc);
@@ -350,7 +338,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
                                                              float* __restrict__ dbias) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
-  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  tile_at(place_of_group(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
   multiply<T>(w, h, 0, m0, n0, 0, g.k, lds, acc);
@@ -429,7 +417,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_product(Operand a, Operand 
                                                              int tiles_n) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
-  tile_of(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  tile_at(place_of_group(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
   const int k0 = blockIdx.y * p.per, k1 = k0 + p.per < p.k ? k0 + p.per : p.k;

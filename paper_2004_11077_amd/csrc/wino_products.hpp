@@ -86,6 +86,20 @@ __device__ __forceinline__ f32x4 multiply_block(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Work group of a grid of `all` -> its place.  Consecutive work groups go round robin over the 8 XCDs;
+// each XCD gets a run of places, so that neighbours share its L2.
+__device__ __forceinline__ int place_of_group(int b, int all) {
+  const int per = all / 8;
+  return b < per * 8 ? (b & 7) * per + (b >> 3) : b;
+}
+// Place -> tile (m, n): bands of eight tiles m, whose rows stay in the L2 while those of n pass.
+__device__ __forceinline__ void tile_at(int b, int tiles_m, int tiles_n, int& m, int& n) {
+  const int band = b / (8 * tiles_n), rest = b - band * 8 * tiles_n;
+  const int wide = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+  m = band * 8 + rest % wide;
+  n = rest / wide;
+}
+
 template <int BM_, int BN_, int WM_, int WN_, int NP_, int RING_, bool AX_ = false, bool BX_ = false>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NP = NP_, RING = RING_;

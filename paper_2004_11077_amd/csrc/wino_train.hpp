@@ -55,7 +55,7 @@ struct UpdateArgs {
 };
 struct UpdateLayout {
   int r, c, rp, cp;           // r <= c: the smaller and the larger side; rounded up to whole lines
-  int splits;                 // ranges of k of A's product
+  int side, splits;           // tiles and ranges of k of A's product
   size_t norms, x, x2, gram, poly, parts, bytes;
 };
 UpdateLayout update_layout(const UpdateArgs& a);

@@ -58,14 +58,14 @@ struct Planes {
   uint16_t* p;
   long batch;
   int ld, e;
-  __device__ __forceinline__ uint16_t* at(int row, int k) const {
-    return p + blockIdx.z * batch + (long)row * ld * 2 + place<2>(k);
+  __device__ __forceinline__ uint16_t* at(int z, int row, int k) const {
+    return p + z * batch + (long)row * ld * 2 + place<2>(k);
   }
 };
 
 // Four consecutive elements of a row, from a multiple of four.
-__device__ __forceinline__ void put(const Planes& o, int row, int k, f32x4 v) {
-  uint16_t* to = o.at(row, k);
+__device__ __forceinline__ void put(const Planes& o, int z, int row, int k, f32x4 v) {
+  uint16_t* to = o.at(z, row, k);
   const float s = power(o.e);
   uint16_t q[4][2];
 #pragma unroll
@@ -75,8 +75,8 @@ __device__ __forceinline__ void put(const Planes& o, int row, int k, f32x4 v) {
     *reinterpret_cast<ushort4*>(to + p * 32) = make_ushort4(q[0][p], q[1][p], q[2][p], q[3][p]);
 }
 // The same four values as one element of four consecutive rows.
-__device__ __forceinline__ void put_across(const Planes& o, int row, int k, int rows, f32x4 v) {
-  uint16_t* to = o.at(row, k);
+__device__ __forceinline__ void put_across(const Planes& o, int z, int row, int k, int rows, f32x4 v) {
+  uint16_t* to = o.at(z, row, k);
   const float s = power(o.e);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256) void k_update_planes(const void* __restrict__ 
       out[0][e] = h[0];
       out[1][e] = h[1];
     }
-    uint16_t* to = x.at(r0 + row, c0 + k);
+    uint16_t* to = x.at(blockIdx.z, r0 + row, c0 + k);
     *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(out[0]);
     *reinterpret_cast<uint4*>(to + 32) = *reinterpret_cast<const uint4*>(out[1]);
   }
@@ -146,18 +146,18 @@ struct Result {
   long o_batch, o_stride;
 };
 
-// Four values D[m .. m + 3][n] of a product of batch blockIdx.z: elements m of the result's row n.
+// Four values D[m .. m + 3][n] of a product of matrix z: elements m of the result's row n.
 // kGram, kPoly: `mirror` writes element n of rows m .. m + 3 as well.  Elements behind the matrix, up to
 // whole lines, become zeros: the next product multiplies them.
 template <Kind KIND>
-__device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, bool mirror) {
+__device__ __forceinline__ void finish(const Result& s, int z, int m, int n, f32x4 v, bool mirror) {
   const float unit = power(-s.e);
 #pragma unroll
   for (int e = 0; e < 4; ++e) v[e] *= unit;
   const int km = KIND <= kPoly ? s.r : s.c;   // rows of the first operand
   if constexpr (KIND == kPoly) {
     if (n < s.r && m < s.gram.ld) {
-      const uint16_t* at = s.gram.at(n, m);
+      const uint16_t* at = s.gram.at(z, n, m);
       const ushort4 h = *reinterpret_cast<const ushort4*>(at), l = *reinterpret_cast<const ushort4*>(at + 32);
       const float one = power(-s.gram.e);
       const float old[4] = {f16_value(h.x) + f16_value(l.x), f16_value(h.y) + f16_value(l.y),
@@ -172,7 +172,7 @@ __device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, b
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (m + e >= s.c) continue;
-      const long at = blockIdx.z * s.o_batch + (s.across ? (long)(m + e) * s.o_stride + n : (long)n * s.o_stride + m + e);
+      const long at = z * s.o_batch + (s.across ? (long)(m + e) * s.o_stride + n : (long)n * s.o_stride + m + e);
       if (s.bf16) static_cast<uint16_t*>(s.o)[at] = bf16_bits(s.scale * v[e]);
       else static_cast<float*>(s.o)[at] = s.scale * v[e];
     }
@@ -181,9 +181,9 @@ __device__ __forceinline__ void finish(const Result& s, int m, int n, f32x4 v, b
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (m + e >= km) k[e] = 0;
-    if (n < s.r && m < s.out.ld) put(s.out, n, m, k);
+    if (n < s.r && m < s.out.ld) put(s.out, z, n, m, k);
     // zeros behind a row of the mirror image come from the tile that holds them unmirrored
-    if (KIND <= kPoly && mirror && n < s.r) put_across(s.out, m, n, s.r, v);
+    if (KIND <= kPoly && mirror && n < s.r) put_across(s.out, z, m, n, s.r, v);
   }
 }
 
@@ -195,19 +195,21 @@ __device__ __forceinline__ void triangle(int i, int& m, int& n) {
   n = i - m * (m + 1) / 2;
 }
 
-// Products of many tiles.  blockIdx.x: tile, .y: range of k, .z: batch.  With several ranges their fp32
-// sums go to `parts` [range][batch][n][m], for k_update_join.
+// Products of many tiles.  blockIdx.x: matrix and tile (`tiles` a matrix), .y: range of k.  With several
+// ranges their fp32 sums go to `parts` [range][matrix][n][m], for k_update_join.
 template <class T, Kind KIND>
-__global__ __launch_bounds__(T::THREADS) void k_update_product(Operand x, Operand y, int k, int per, int tiles_m,
-                                                               Result s, float* __restrict__ parts, long part,
-                                                               int part_ld) {
+__global__ __launch_bounds__(T::THREADS) void k_update_product(Operand x, Operand y, int k, int per, int tiles,
+                                                               int tiles_m, Result s, float* __restrict__ parts,
+                                                               long part, int part_ld) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
-  int tm = blockIdx.x % tiles_m, tn = blockIdx.x / tiles_m;
-  if constexpr (KIND <= kPoly) triangle(blockIdx.x, tm, tn);
+  const int at = place_of_group(blockIdx.x, gridDim.x), z = at / tiles;
+  int tm, tn;
+  if constexpr (KIND <= kPoly) triangle(at - z * tiles, tm, tn);
+  else tile_at(at - z * tiles, tiles_m, tiles / tiles_m, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   const int k0 = blockIdx.y * per, k1 = k0 + per < k ? k0 + per : k;
   f32x4 acc[T::TM][T::TN] = {};
-  multiply<T>(x, y, blockIdx.z, m0, n0, k0, k1, lds, acc);
+  multiply<T>(x, y, z, m0, n0, k0, k1, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
 #pragma unroll
@@ -218,9 +220,9 @@ __global__ __launch_bounds__(T::THREADS) void k_update_product(Operand x, Operan
       const int m = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4;
       if (parts) {
         if (n < s.r && m < part_ld)
-          *reinterpret_cast<f32x4*>(parts + blockIdx.y * part + ((long)blockIdx.z * s.r + n) * part_ld + m) = acc[i][j];
+          *reinterpret_cast<f32x4*>(parts + blockIdx.y * part + ((long)z * s.r + n) * part_ld + m) = acc[i][j];
       } else {
-        finish<KIND>(s, m, n, acc[i][j], tm != tn);
+        finish<KIND>(s, z, m, n, acc[i][j], tm != tn);
       }
     }
   }
@@ -240,7 +242,7 @@ __global__ __launch_bounds__(256) void k_update_join(const float* __restrict__ p
     if (n < s.r && m < part_ld)
       for (int q = 0; q < count; ++q)
         v += *reinterpret_cast<const f32x4*>(parts + q * part + ((long)blockIdx.z * s.r + n) * part_ld + m);
-    finish<KIND>(s, m, n, v, tm != tn);
+    finish<KIND>(s, blockIdx.z, m, n, v, tm != tn);
   }
 }
 
@@ -249,12 +251,15 @@ template <Kind KIND, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_update_few(Operand x, int k, int tiles, Result s) {
   typedef Few<2, WAVES> T;
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
-  const int m0 = blockIdx.x % tiles * 32, n0 = blockIdx.x / tiles * 32;
+  const int at = place_of_group(blockIdx.x, gridDim.x), z = at / tiles;
+  int tm, tn;
+  triangle(at - z * tiles, tm, tn);
   f32x4 acc[1][1] = {};
-  multiply<T>(x, x, blockIdx.z, m0, n0, 0, k, lds, acc);
+  multiply<T>(x, x, z, tm * 32, tn * 32, 0, k, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (wave >= 4) return;
-  finish<KIND>(s, m0 + (wave & 1) * 16 + (lane >> 4) * 4, n0 + (wave >> 1) * 16 + (lane & 15), acc[0][0], false);
+  finish<KIND>(s, z, tm * 32 + (wave & 1) * 16 + (lane >> 4) * 4, tn * 32 + (wave >> 1) * 16 + (lane & 15), acc[0][0],
+               tm != tn);
 }
 
 // Tiles of products; AX: k across the rows of the first operand (X in P X).
@@ -277,31 +282,31 @@ void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& 
   if constexpr (KIND <= kPoly) {
     if (few(l, batch)) {
       // eight waves where four would have more than four lines of k each
-      const int tm = tiles_of(l.r, 32);
-      const dim3 grid(tm * tm, 1, batch);
+      const int tm = half_of(tiles_of(l.r, 32));
+      const dim3 grid(tm * batch);
       if (k > 32 * 4 * 4) wino_launch((k_update_few<KIND, 8>), grid, dim3(512), st, x, k, tm, s);
       else wino_launch((k_update_few<KIND, 4>), grid, dim3(256), st, x, k, tm, s);
       return;
     }
     const auto go = [&](auto tile) {
       typedef decltype(tile) T;
-      const int tm = tiles_of(l.r, T::BM), splits = KIND == kGram ? l.splits : 1;
+      const int tiles = half_of(tiles_of(l.r, T::BM)), splits = KIND == kGram ? l.splits : 1;
       const int per = (int)up((k + splits - 1) / splits, 32);
       const long part = (long)batch * l.r * l.rp;
-      wino_launch((k_update_product<T, KIND>), dim3(half_of(tm), splits, batch), dim3(T::THREADS), st, x, y, k, per, tm,
-                  s, splits > 1 ? parts : nullptr, part, l.rp);
+      wino_launch((k_update_product<T, KIND>), dim3(tiles * batch, splits), dim3(T::THREADS), st, x, y, k, per,
+                  tiles, 0, s, splits > 1 ? parts : nullptr, part, l.rp);
       if (splits > 1)
         wino_launch((k_update_join<KIND>), dim3(half_of(tiles_of(l.rp, 64)), 1, batch), dim3(256), st,
                     (const float*)parts, splits, part, l.rp, s);
     };
-    if (half_of(tiles_of(l.r, 128)) * batch >= 512) go(Tiles<false>::Mid{});
+    if (l.side == 128 && KIND == kGram) go(Tiles<false>::Mid{});
     else go(Tiles<false>::Small{});
   } else {
     const auto go = [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = tiles_of(l.c, T::BM), tn = tiles_of(l.r, T::BN);
-      wino_launch((k_update_product<T, KIND>), dim3(tm * tn, 1, batch), dim3(T::THREADS), st, x, y, k, k, tm, s,
-                  (float*)nullptr, 0L, 0);
+      wino_launch((k_update_product<T, KIND>), dim3(tm * tn * batch), dim3(T::THREADS), st, x, y, k, k, tm * tn, tm,
+                  s, (float*)nullptr, 0L, 0);
     };
     const auto count = [&](int side) { return (long)tiles_of(l.c, side) * tiles_of(l.r, side) * batch; };
     if (count(256) >= 512) go(Tiles<true>::Big{});
@@ -337,9 +342,10 @@ UpdateLayout update_layout(const UpdateArgs& a) {
   l.poly = take(item * l.r * l.rp);
   l.splits = 1;
   if (a.batch && l.r && !few(l, a.batch)) {
-    // ranges of A's k until its tiles of 64 x 64 fill the chip, each of 512 or more
-    const long tiles = (long)half_of(tiles_of(l.r, 64)) * a.batch;
-    long s = 512 / tiles;
+    // ranges of A's k until its tiles fill the chip, each of 512 or more
+    l.side = (long)half_of(tiles_of(l.r, 128)) * a.batch >= 64 ? 128 : 64;
+    const long tiles = (long)half_of(tiles_of(l.r, l.side)) * a.batch;
+    long s = (512 + tiles / 2) / tiles;
     if (s > l.cp / 512) s = l.cp / 512;
     l.splits = (int)(s < 1 ? 1 : s);
     if (l.splits > 1) l.parts = take(4 * (size_t)l.splits * a.batch * l.r * l.rp);
