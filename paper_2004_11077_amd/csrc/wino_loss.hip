@@ -508,13 +508,10 @@ struct Tiles {
   typedef Tile<64, 64, 2, 2, NP, 2, AX, BX> Small;
 };
 long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
-int side_for(long m, long n, long splits = 1) {
-  return count_of(m, n, 256) * splits >= 512 ? 256 : count_of(m, n, 128) * splits >= 256 ? 128 : 64;
-}
 // The same of products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the
 // waves where there are few tiles.
 int side_along(long m, long n, long k) {
-  const int side = side_for(m, n);
+  const int side = side_for(m, n, 1);
   return side == 64 && count_of(m, n, 64) < 64 && k >= 256 ? 32 : side;
 }
 constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
@@ -644,7 +641,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
       const int tk = (int)up(a.rows, 64);
       Product p{const_cast<void*>(row_at(a, dw, first, a.features)), a.features, 0, a.bf16, tk, tk, a.features, q.count,
                 ref, &num->of_h};
-      with_tile<NP, true, true>(side_for(a.features, q.count), [&](auto tile) {
+      with_tile<NP, true, true>(side_for(a.features, q.count, 1), [&](auto tile) {
         typedef decltype(tile) T;
         const int tm = (a.features + T::BM - 1) / T::BM, tn = (q.count + T::BN - 1) / T::BN;
         wino_launch((k_loss_product<T>), dim3(tm * tn), dim3(T::THREADS), st, oh, od, p, tm, tn);
@@ -683,7 +680,7 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
   l.splits = 1;
   if (!back) {
     // pieces are whole multiples of 256 classes, so no tile spans two
-    const size_t least = T >= 512 * 256 ? 256 : T >= 256 * 128 ? 128 : T >= 64 * 64 ? 64 : 32;   // of side_along() for any classes
+    const size_t least = T >= 64 * 64 ? 64 : 32;   // of side_along() for any classes
     l.parts = take(8 * T * (up(V, 256) / least));
     l.target = take(4 * T);
     l.unit_w = take(4 * P);
@@ -691,14 +688,18 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
   } else {
     l.dl = take(item * T * vp);
     l.side = side_along((long)P, (long)T, l.dp);
-    // ranges of classes until dh's tiles fill the chip, each of 512 classes or more
+    // ranges of classes, each of 512 or more, until dh's tiles fill the chip: one tile of 256 a compute
+    // unit, or two of the smaller ones
     const long room = (long)(vp / 512 ? vp / 512 : 1);
-    l.dh_side = count_of((long)D, (long)T, 256) >= 100 ? 256 : side_for((long)D, (long)T, room < 8 ? room : 8);
-    const long tiles = T ? count_of((long)D, (long)T, l.dh_side) : 1;
-    const long full = l.dh_side == 256 ? 256 : 512;
-    long s = (full + tiles - 1) / tiles;
-    if (s > room) s = room;
-    l.splits = (int)(s < 1 ? 1 : s);
+    double most = 0;
+    for (int side = 256; side >= 64 && T; side /= 2) {
+      const long tiles = count_of((long)D, (long)T, side), slots = side == 256 ? 256 : 512;
+      long ranges = slots / tiles;
+      ranges = ranges > room ? room : ranges < 1 ? 1 : ranges;
+      const double rate = side == 256 ? 1.0 : side == 128 ? 0.93 : 0.85;
+      const double score = rate * D * T * ranges / ((double)((tiles * ranges + 255) / 256) * 256 * side * side);
+      if (score > most) most = score, l.dh_side = side, l.splits = (int)ranges;
+    }
     l.dh = take(4 * T * D * l.splits);
     l.dbias = take(4 * V * waves_n(l.side) * (T ? (T + l.side - 1) / l.side : 1));
   }

@@ -86,6 +86,22 @@ __device__ __forceinline__ f32x4 multiply_block(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Side of the square tiles (256, 128 or 64) for `z` products of m x n: the one that leaves least of the
+// chip idle, counting what of its tiles lies outside, compute units that wait for the others' last tile, and
+// the rates that tiles reach when nothing is idle (of the 256 x 256 ones; 10112 x 1024 x 576 and 16384 x 2048
+// x 4096: 1421, 1297 and about 1200 TFLOP/s).
+inline int side_for(double m, double n, double z) {
+  int best = 64;
+  double most = 0;
+  for (int side = 256; side >= 64; side /= 2) {
+    const double tiles = __builtin_ceil(m / side) * __builtin_ceil(n / side) * z;
+    const double rate = side == 256 ? 1.0 : side == 128 ? 0.93 : 0.85;
+    const double score = rate * m * n * z / (__builtin_ceil(tiles / 256) * 256 * side * side);
+    if (score > most) most = score, best = side;
+  }
+  return best;
+}
+
 // Work group of a grid of `all` -> its place.  Consecutive work groups go round robin over the 8 XCDs;
 // each XCD gets a run of places, so that neighbours share its L2.
 __device__ __forceinline__ int place_of_group(int b, int all) {

@@ -273,14 +273,15 @@ struct Tiles {
 int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
 int half_of(int tiles) { return tiles * (tiles + 1) / 2; }
 
-// Few rows: the symmetric products' tiles of 128 would leave most of the chip idle.
-bool few(const UpdateLayout& l, int batch) { return (long)l.r * l.r * batch <= 256L * 256 * 4; }
+// Symmetric products of few tiles and not many k: no barriers, one launch.  (3 matrices of 256 rows, k of
+// 2304: 20.9 us, against ? in ranges with a join.)
+bool few(const UpdateLayout& l, int batch, int k) { return (long)l.r * l.r * batch <= 256L * 256 * 4 && k <= 1024; }
 
 template <Kind KIND>
 void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& y, int k, const Result& s,
              float* parts, hipStream_t st) {
   if constexpr (KIND <= kPoly) {
-    if (few(l, batch)) {
+    if (few(l, batch, k)) {
       // eight waves where four would have more than four lines of k each
       const int tm = half_of(tiles_of(l.r, 32));
       const dim3 grid(tm * batch);
@@ -308,9 +309,9 @@ void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& 
       wino_launch((k_update_product<T, KIND>), dim3(tm * tn * batch), dim3(T::THREADS), st, x, y, k, k, tm * tn, tm,
                   s, (float*)nullptr, 0L, 0);
     };
-    const auto count = [&](int side) { return (long)tiles_of(l.c, side) * tiles_of(l.r, side) * batch; };
-    if (count(256) >= 512) go(Tiles<true>::Big{});
-    else if (count(128) >= 192) go(Tiles<true>::Mid{});
+    const int side = side_for(l.c, l.r, batch);
+    if (side == 256) go(Tiles<true>::Big{});
+    else if (side == 128) go(Tiles<true>::Mid{});
     else go(Tiles<true>::Small{});
   }
 }
@@ -341,7 +342,7 @@ UpdateLayout update_layout(const UpdateArgs& a) {
   l.gram = take(item * l.r * l.rp);
   l.poly = take(item * l.r * l.rp);
   l.splits = 1;
-  if (a.batch && l.r && !few(l, a.batch)) {
+  if (a.batch && l.r && !few(l, a.batch, (int)up(l.c, 32))) {
     // ranges of A's k until its tiles fill the chip, each of 512 or more
     l.side = (long)half_of(tiles_of(l.r, 128)) * a.batch >= 64 ? 128 : 64;
     const long tiles = (long)half_of(tiles_of(l.r, l.side)) * a.batch;
