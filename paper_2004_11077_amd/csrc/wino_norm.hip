@@ -95,13 +95,40 @@ __device__ __forceinline__ F sum_lanes(F v, F* lds) {
 
 template <int LANES>
 constexpr int kThreads = LANES > 256 ? LANES : 256;
+// Backward pass: sixteen waves a work group where their sums of columns fit 32 KiB of LDS.
+template <int LANES, int PER>
+constexpr int kBackThreads = LANES > 256 ? LANES : PER <= 8 ? 1024 : PER <= 16 ? 512 : 256;
 
-// One value to its output type; F is double exactly where the type is int8.
-template <class F>
-__device__ __forceinline__ int code_of(F y, float s_y) {
-  F q = __builtin_rint(y / (F)s_y);
+// Both sums over the LANES lanes of a row; `lds`: a float2 per wave, another buffer than in the call
+// before, so that one barrier is enough.
+template <int LANES>
+__device__ __forceinline__ void sum_pair(float& a, float& b, float2* lds) {
+#pragma unroll
+  for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) a += __shfl_xor(a, d, 64), b += __shfl_xor(b, d, 64);
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    const float2* mine = lds + threadIdx.x / LANES * (LANES / 64);
+    a = mine[0].x, b = mine[0].y;
+#pragma unroll
+    for (int w = 1; w < LANES / 64; ++w) a += mine[w].x, b += mine[w].y;
+  }
+}
+
+// A code; F is double exactly where these come out.
+__device__ __forceinline__ int code_of(double y) {
+  double q = __builtin_rint(y);
   q = q > 127 ? 127 : q < -127 ? -127 : q;
   return (int)q;   // a NaN gives 0
+}
+
+// 1 / sqrt(v).  64 bits: the instruction's 26 bits and two steps of r <- r (3 - v r r) / 2.
+__device__ __forceinline__ float inverse_root(float v) { return 1.f / __builtin_sqrtf(v); }
+__device__ __forceinline__ double inverse_root(double v) {
+  double r = __builtin_amdgcn_rsq(v);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) r = r * __builtin_fma(-0.5 * v * r, r, 1.5);
+  return r;
 }
 
 template <class TI, class F, int LANES, int VEC, int NV>
@@ -130,7 +157,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void k_norm(NormArgs a, const TI* 
 #pragma unroll
     for (int e = 0; e < VEC; ++e) sum += (F)v[i][e];
   }
-  const F mu = sum_lanes<LANES>(sum, lds) / (F)C;
+  const F mu = sum_lanes<LANES>(sum, lds) * (F)a.inv_c;
   F sq = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -141,8 +168,8 @@ __global__ __launch_bounds__(kThreads<LANES>) void k_norm(NormArgs a, const TI* 
       sq = __builtin_elementwise_fma(d, d, sq);
     }
   }
-  const F var = sum_lanes<LANES>(sq, lds) / (F)C;
-  const F s = (F)1 / __builtin_elementwise_sqrt(var + (F)a.eps);
+  const F var = sum_lanes<LANES>(sq, lds) * (F)a.inv_c;
+  const F s = inverse_root(var + (F)a.eps);
   if (!live) continue;   // no other lane of this row's work group waits for these
   if (lane == 0) {
     if (mean) mean[row] = (float)mu;
@@ -162,7 +189,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void k_norm(NormArgs a, const TI* 
       int q[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        q[e] = code_of<F>(((F)v[i][e] - mu) * s * (F)ga[e] + (F)be[e], a.s_y);
+        q[e] = code_of((((F)v[i][e] - mu) * s * (F)ga[e] + (F)be[e]) * a.inv_s);
       store<VEC>(static_cast<int8_t*>(y) + at, q);
     } else {
 #pragma unroll
@@ -185,14 +212,14 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a, const TI* __rest
   const TI* px = x + row * a.x_stride;
   F sum = 0;
   for (int c = threadIdx.x; c < a.channels; c += 1024) sum += (F)widen(px[c]);
-  const F mu = sum_lanes<1024>(sum, lds) / (F)a.channels;
+  const F mu = sum_lanes<1024>(sum, lds) * (F)a.inv_c;
   F sq = 0;
   for (int c = threadIdx.x; c < a.channels; c += 1024) {
     const F d = (F)widen(px[c]) - mu;
     sq = __builtin_elementwise_fma(d, d, sq);
   }
-  const F var = sum_lanes<1024>(sq, lds) / (F)a.channels;
-  const F s = (F)1 / __builtin_elementwise_sqrt(var + (F)a.eps);
+  const F var = sum_lanes<1024>(sq, lds) * (F)a.inv_c;
+  const F s = inverse_root(var + (F)a.eps);
   if (threadIdx.x == 0) {
     if (mean) mean[row] = (float)mu;
     if (rstd) rstd[row] = (float)s;
@@ -202,7 +229,7 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a, const TI* __rest
     const long at = row * a.y_stride + c;
     const F v = ((F)widen(px[c]) - mu) * s;
     if constexpr (sizeof(F) == 8) {
-      static_cast<int8_t*>(y)[at] = (int8_t)code_of<F>(v * ga + be, a.s_y);
+      static_cast<int8_t*>(y)[at] = (int8_t)code_of((v * ga + be) * a.inv_s);
     } else {
       const float o[1] = {__builtin_fmaf(v, ga, be)};
       if (a.y_type == kF32) store<1>(static_cast<float*>(y) + at, o);
@@ -212,58 +239,87 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a, const TI* __rest
   }
 }
 
+// Values as they lie in memory, widened when they are used: the next row's are under way while this
+// one's sums are taken.
+template <class T, int VEC>
+struct Raw {
+  vec_of<T, VEC> v;
+  __device__ __forceinline__ float operator[](int e) const { return v[e]; }
+  __device__ __forceinline__ void fill(float x) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = x;
+  }
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VEC == 1) v[0] = *p;
+    else v = *reinterpret_cast<const vec_of<T, VEC>*>(p);
+  }
+};
+template <int VEC>
+struct Raw<bf16_t, VEC> {
+  vec_of<uint16_t, VEC> v;
+  __device__ __forceinline__ float operator[](int e) const { return widen(bf16_t{v[e]}); }
+  __device__ __forceinline__ void load(const bf16_t* p) {
+    if constexpr (VEC == 1) v[0] = p->bits;
+    else v = *reinterpret_cast<const vec_of<uint16_t, VEC>*>(p);
+  }
+};
+
 // Backward pass.  A work group takes every gridDim-th set of rows; its lanes keep their channels' sums
 // of dy xh and dy in registers over all its rows, joins the sets of a work group in LDS and leaves one
 // partial sum per work group: no atomics, so the order of the sums is fixed.
 template <class TI, class TG, int LANES, int VEC, int NV>
-__global__ __launch_bounds__(kThreads<LANES>) void k_norm_backward(
+__global__ __launch_bounds__((kBackThreads<LANES, NV * VEC>)) void k_norm_backward(
     NormArgs a, const TG* __restrict__ dy, const TI* __restrict__ x, const float* __restrict__ gamma,
     const float* __restrict__ mean, const float* __restrict__ rstd, TG* __restrict__ dx,
     float* __restrict__ parts) {
-  __shared__ float lds[16], lds2[16];
-  constexpr int ROWS = kThreads<LANES> / LANES;
+  __shared__ float2 lds[2][16];
+  constexpr int THREADS = kBackThreads<LANES, NV * VEC>, ROWS = THREADS / LANES;
+  int turn = 0;
   const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
   const int C = a.channels;
-  float ga[NV][VEC], dg[NV][VEC], db[NV][VEC];
+  float dg[NV][VEC] = {}, db[NV][VEC] = {};
+  const float inv_c = (float)a.inv_c;
+  Raw<TI, VEC> nx[NV];
+  Raw<TG, VEC> ng[NV];
+  float next_mu = 0, next_s = 0;
+  const auto fetch = [&](long row) {
+    if (row >= a.rows) return;
+    next_mu = mean[row], next_s = rstd[row];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (i * LANES + lane) * VEC;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) ga[i][e] = 1, dg[i][e] = 0, db[i][e] = 0;
-    if (gamma && c < C) load<VEC>(gamma + c, ga[i]);
-  }
-  const float inv_c = 1.f / (float)C;
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * LANES + lane) * VEC;
+      if (c < C) nx[i].load(x + row * a.x_stride + c), ng[i].load(dy + row * a.dy_stride + c);
+    }
+  };
+  fetch((long)blockIdx.x * ROWS + sub);
   for (long first = (long)blockIdx.x * ROWS; first < a.rows; first += (long)gridDim.x * ROWS) {
     const long row = first + sub;
     const bool live = row < a.rows;
+    const float mu = next_mu, s = next_s;
     float vx[NV][VEC], vg[NV][VEC];
-    const float mu = live ? mean[row] : 0, s = live ? rstd[row] : 0;
     float s1 = 0, s2 = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * LANES + lane) * VEC;
-      if (live && c < C) {
-        load<VEC>(x + row * a.x_stride + c, vx[i]);
-        load<VEC>(dy + row * a.dy_stride + c, vg[i]);
-      } else {
+      const bool in = live && c < C;
+      float ga[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) vx[i][e] = mu, vg[i][e] = 0;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int e = 0; e < VEC; ++e) ga[e] = 1;
+      if (gamma && c < C) load<VEC>(gamma + c, ga);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float xh = (vx[i][e] - mu) * s, d = vg[i][e];
+        const float xh = in ? (nx[i][e] - mu) * s : 0.f, d = in ? ng[i][e] : 0.f;
         dg[i][e] = __builtin_fmaf(d, xh, dg[i][e]);
         db[i][e] += d;
         vx[i][e] = xh;
-        vg[i][e] = d * ga[i][e];
+        vg[i][e] = d * ga[e];
         s1 += vg[i][e];
         s2 = __builtin_fmaf(vg[i][e], xh, s2);
       }
-    s1 = sum_lanes<LANES>(s1, lds) * inv_c;
-    s2 = sum_lanes<LANES>(s2, lds2) * inv_c;
+    }
+    fetch(row + (long)gridDim.x * ROWS);
+    sum_pair<LANES>(s1, s2, lds[turn ^= 1]);
+    s1 *= inv_c, s2 *= inv_c;
     if (live && dx) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -278,7 +334,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void k_norm_backward(
   if (!parts) return;
   float* out = parts + (long)blockIdx.x * 2 * C;
   if constexpr (ROWS > 1) {
-    __shared__ float join[256 * NV * VEC];   // [set of rows][vector][lane][element]
+    __shared__ float join[THREADS * NV * VEC];   // [set of rows][vector][lane][element]
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
       __syncthreads();
@@ -288,7 +344,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void k_norm_backward(
         for (int e = 0; e < VEC; ++e)
           join[sub * LANES * NV * VEC + (i * LANES + lane) * VEC + e] = which ? db[i][e] : dg[i][e];
       __syncthreads();
-      for (int c = threadIdx.x; c < C; c += 256) {
+      for (int c = threadIdx.x; c < C; c += THREADS) {
         float v = join[c];
 #pragma unroll 4
         for (int q = 1; q < ROWS; ++q) v += join[q * LANES * NV * VEC + c];
@@ -315,7 +371,7 @@ __global__ __launch_bounds__(1024) void k_norm_backward_long(
   for (long row = blockIdx.x; row < a.rows; row += gridDim.x) {
   const TI* px = x + row * a.x_stride;
   const TG* pg = dy + row * a.dy_stride;
-  const float mu = mean[row], s = rstd[row], inv_c = 1.f / (float)a.channels;
+  const float mu = mean[row], s = rstd[row], inv_c = (float)a.inv_c;
   float s1 = 0, s2 = 0;
   for (int c = threadIdx.x; c < a.channels; c += 1024) {
     const float g = widen(pg[c]) * (gamma ? gamma[c] : 1.f), xh = (widen(px[c]) - mu) * s;
@@ -351,25 +407,27 @@ __global__ __launch_bounds__(256) void k_norm_columns_long(NormArgs a, const TG*
   out[a.channels + c] = db;
 }
 
-// Partial sums [parts][2][C] -> dgamma, dbeta.  64 channels a work group, 16 threads each.
+// Partial sums [parts][2][C] -> dgamma, dbeta.  16 channels a work group, 64 threads each.
 __global__ __launch_bounds__(1024) void k_norm_join(const float* __restrict__ parts, int count, int C,
                                                     float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ float lds[16][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + lane;   // of 2 C
+  __shared__ float lds[64][16];
+  const int x = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int c = blockIdx.x * 16 + x;   // of 2 C
   float v = 0;
   if (c < 2 * C)
-#pragma unroll 4
-    for (int p = g; p < count; p += 16) v += parts[(long)p * 2 * C + c];
-  lds[g][lane] = v;
+#pragma unroll 8
+    for (int p = g; p < count; p += 64) v += parts[(long)p * 2 * C + c];
+  lds[g][x] = v;
   __syncthreads();
+  for (int d = 32; d > 0; d /= 2) {
+    if (g < d) lds[g][x] += lds[g + d][x];
+    __syncthreads();
+  }
   if (g == 0 && c < 2 * C) {
-#pragma unroll
-    for (int q = 1; q < 16; ++q) v += lds[q][lane];
     if (c < C) {
-      if (dgamma) dgamma[c] = v;
+      if (dgamma) dgamma[c] = lds[0][x];
     } else if (dbeta) {
-      dbeta[c - C] = v;
+      dbeta[c - C] = lds[0][x];
     }
   }
 }
@@ -384,7 +442,7 @@ bool at(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 template <class F>
 bool with_shape(long n, F&& f) {
 #define SHAPE(L, V) if (n <= L * V) { f(std::integral_constant<int, L>{}, std::integral_constant<int, V>{}); return true; }
-  SHAPE(4, 1) SHAPE(16, 1) SHAPE(16, 2) SHAPE(64, 1) SHAPE(64, 2) SHAPE(64, 4) SHAPE(256, 2) SHAPE(256, 4) SHAPE(1024, 2)
+  SHAPE(4, 1) SHAPE(16, 1) SHAPE(16, 2) SHAPE(64, 1) SHAPE(64, 2) SHAPE(64, 4) SHAPE(256, 2) SHAPE(256, 4) SHAPE(512, 4)
 #undef SHAPE
   return false;
 }
@@ -423,8 +481,8 @@ hipError_t norm_backward(const NormArgs& a, const TG* dy, const TI* x, const flo
     constexpr int VEC = decltype(vec)::value;
     return with_shape(a.channels / VEC, [&](auto lanes, auto nv) {
       constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
-      wino_launch((k_norm_backward<TI, TG, L, VEC, NV>), dim3(count), dim3(kThreads<L>), st, a, dy, x, gamma,
-                  mean, rstd, dx, to);
+      wino_launch((k_norm_backward<TI, TG, L, VEC, NV>), dim3(count), dim3(kBackThreads<L, NV * VEC>), st, a, dy,
+                  x, gamma, mean, rstd, dx, to);
     });
   };
   if (!(whole ? go(std::integral_constant<int, V>{}) : go(std::integral_constant<int, 1>{}))) {
@@ -436,7 +494,7 @@ hipError_t norm_backward(const NormArgs& a, const TG* dy, const TI* x, const flo
                   mean, rstd, to);
   }
   if (sums)
-    wino_launch(k_norm_join, dim3((2 * a.channels + 63) / 64), dim3(1024), st, (const float*)parts, count,
+    wino_launch(k_norm_join, dim3((2 * a.channels + 15) / 16), dim3(1024), st, (const float*)parts, count,
                 a.channels, dgamma, dbeta);
   return hipGetLastError();
 }

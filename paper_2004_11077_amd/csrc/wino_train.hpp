@@ -14,7 +14,8 @@ inline size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 struct NormArgs {
   long rows;
   int channels, x_type, y_type, g_type;
-  float eps, s_y;
+  float eps;
+  double inv_s, inv_c;    // 1 / s_y, 1 / channels
   long x_stride, y_stride, dy_stride, dx_stride;
 };
 hipError_t launch_norm(const NormArgs& a, const void* x, const float* gamma, const float* beta, void* y,
