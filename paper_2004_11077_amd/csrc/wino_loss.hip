@@ -46,7 +46,7 @@ __device__ __forceinline__ int exponent_for(float most) {
   return most == 0.f ? 0 : e > 120 ? 120 : e;
 }
 
-// Maximum over the 256 threads of a work group.
+// Maximum over the threads of a work group; lds: one value per wave.
 __device__ __forceinline__ float group_max(float m, float* lds) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
@@ -79,25 +79,25 @@ __device__ __forceinline__ float range_of(const float* x, long ld, int rows, int
   if (!g && ld == cols) {   // one run of values
     const long items = (long)rows * cols;
 #pragma unroll 8
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += kRange * 256) take(x[i]);
+    for (long i = (long)blockIdx.x * 1024 + threadIdx.x; i < items; i += kRange * 1024) take(x[i]);
   } else {
     for (int r = blockIdx.x; r < rows; r += kRange) {
       if (g && !g->kept(r)) continue;
-      for (int c = threadIdx.x; c < cols; c += 256) take(x[(long)r * ld + c]);
+      for (int c = threadIdx.x; c < cols; c += 1024) take(x[(long)r * ld + c]);
     }
   }
   return group_max(m, lds);
 }
 
-// First kernel of a call: the largest |dloss| of the rows that count, and for fp32 the ranges of W and
+// First kernel of a backward pass: the largest |dloss| of the rows that count, and for fp32 the ranges of W and
 // of h's rows that count.
-__global__ __launch_bounds__(256) void k_loss_range(const float* __restrict__ w, long w_ld,
-                                                    const float* __restrict__ h, long h_ld, int features, Rows g,
-                                                    const float* __restrict__ dloss, Numbers* __restrict__ to) {
-  __shared__ float lds[4];
+__global__ __launch_bounds__(1024) void k_loss_range(const float* __restrict__ w, long w_ld,
+                                                     const float* __restrict__ h, long h_ld, int features, Rows g,
+                                                     const float* __restrict__ dloss, Numbers* __restrict__ to) {
+  __shared__ float lds[16];
   if (dloss && blockIdx.x == 0) {
     float m = 0;
-    for (int t = threadIdx.x; t < g.rows; t += 256)
+    for (int t = threadIdx.x; t < g.rows; t += 1024)
       if (g.kept(t)) m = __builtin_fmaxf(m, __builtin_fabsf(dloss[t]));
     m = group_max(m, lds);
     if (threadIdx.x == 0) to->ref = m;
@@ -229,12 +229,24 @@ __device__ __forceinline__ void to_logits(const Logits& g, int v0, int j_t, f32x
   }
 }
 
+// A row's lse from its maximum and its sum of exponentials, and its loss from that and its target's logit.
+__device__ __forceinline__ void finish_row(const Rows& g, int t, float top, float sum, const float* hit, float* loss,
+                                           float* lse) {
+  const float all = (top == -kInf ? 0.f : top) + __builtin_logf(sum);   // log 0 = -inf: every class masked
+  lse[t] = all;
+  float v = 0;
+  if (g.kept(t)) v = hit[t] == -kInf && !(all != all) ? kInf : all - hit[t];
+  loss[t] = v;
+}
+
 // Forward: best[part][t], part = tile of classes: maximum and sum of exp(l - maximum); the target's
-// logit of every row that has one.
+// logit of every row that has one.  With one tile of classes in all (loss given) the rows are finished
+// here.
 template <class T>
 __global__ __launch_bounds__(T::THREADS) void k_loss_logits(Operand w, Operand h, Logits g, int tiles_m,
                                                             int tiles_n, int part0, float2* __restrict__ best,
-                                                            float* __restrict__ hit) {
+                                                            float* hit, float* __restrict__ loss,
+                                                            float* __restrict__ lse) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
   tile_at(place_of_group(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
@@ -285,7 +297,9 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_logits(Operand w, Operand h
     const float base = top == -kInf ? 0.f : top;
 #pragma unroll
     for (int q = 0; q < T::WM; ++q) sum += join[q * T::BN + i].y * exp_of(join[q * T::BN + i].x - base);
-    if (n0 + i < g.g.rows) best[(long)(part0 + tm) * g.g.rows + n0 + i] = make_float2(top, sum);
+    if (n0 + i >= g.g.rows) continue;
+    if (loss) finish_row(g.g, n0 + i, top, sum, hit, loss, lse);   // hit: written before the barrier
+    else best[(long)(part0 + tm) * g.g.rows + n0 + i] = make_float2(top, sum);
   }
 }
 
@@ -321,11 +335,7 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* __restrict__ be
     __syncthreads();
   }
   if (y != 0 || t >= g.rows) return;
-  const float all = base + __builtin_logf(lds[1][0][x]);   // log 0 = -inf: every class masked
-  lse[t] = all;
-  float v = 0;
-  if (g.kept(t)) v = hit[t] == -kInf && !(all != all) ? kInf : all - hit[t];
-  loss[t] = v;
+  finish_row(g, t, top, lds[1][0][x], hit, loss, lse);
 }
 
 // Backward: dl / ref of a piece, rows [t][ld]; the sums over a wave's rows for dbias.
@@ -402,66 +412,85 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
     }
 }
 
-// out[n][m] = sum_k A(m, k) B(n, k): the gradient of row n of W resp. h over its features m.
+// The gradient of the rows of h or W: out[row][f] = sum_k A(row, k) B(f, k) over the features f.
 // kind 0: to fp32, 1: to bf16, both times ref; 2: to fp32 sums of a range of k (blockIdx.y), kept as
-// they are, 3: added to what is there.
+// they are, 3: added to what is there.  A lane of the instruction's result holds four consecutive m of
+// one n.  FOUR: m are the features, four of them one store (rows of out start on whole fours); otherwise
+// m are the rows, and sixteen lanes store neighbouring features.  (dW of 65536 x 2048 in bf16: 585 us and
+// 640; of 10007 x 515 in fp32, whose rows start anywhere: 60 and 55.)
 struct Product {
+  Operand rows, features;
   void* out;
-  long ld, split;        // elements between rows and between ranges of k
+  long split;            // elements between ranges of k
   int kind, k, per;      // k in all and per range
-  int m, n;              // features and rows
+  int count, width;      // rows and features of out
   const float *ref, *unit;
 };
-template <class T>
-__global__ __launch_bounds__(T::THREADS) void k_loss_product(Operand a, Operand b, Product p, int tiles_m,
-                                                             int tiles_n) {
-  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+template <class T, bool FOUR>
+__device__ __forceinline__ void make_product(const Product& p, int group, int groups, int range, char* lds) {
+  const Operand& a = FOUR ? p.features : p.rows;
+  const Operand& b = FOUR ? p.rows : p.features;
+  const int all_m = FOUR ? p.width : p.count, all_n = FOUR ? p.count : p.width;
   int tm, tn;
-  tile_at(place_of_group(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
+  tile_at(place_of_group(group, groups), (all_m + T::BM - 1) / T::BM, (all_n + T::BN - 1) / T::BN, tm, tn);
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
-  const int k0 = blockIdx.y * p.per, k1 = k0 + p.per < p.k ? k0 + p.per : p.k;
+  const int k0 = range * p.per, k1 = k0 + p.per < p.k ? k0 + p.per : p.k;
   multiply<T>(a, b, 0, m0, n0, k0, k1, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
-  float scale = p.kind < 2 ? *p.ref : 1.f;
+  const float scale = p.kind < 2 ? *p.ref : 1.f;
   float unit = 1.f;
   if constexpr (T::NP == 2) unit = *p.unit * (1.f / (1 << kDlExponent));
-  const bool whole = (p.ld & 3) == 0;   // rows of out start on four elements
+  const long base = range * p.split;
 #pragma unroll
-  for (int j = 0; j < T::TN; ++j) {
-    const int n = n0 + (wn * T::TN + j) * 16 + (lane & 15);
-    if (n >= p.n) continue;
+  for (int i = 0; i < T::TM; ++i) {
+    const int m = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4;
+    if (m >= all_m) continue;
 #pragma unroll
-    for (int i = 0; i < T::TM; ++i) {
-      const int m = m0 + (wm * T::TM + i) * 16 + (lane >> 4) * 4;
-      if (m >= p.m) continue;
-      const long at = blockIdx.y * p.split + (long)n * p.ld + m;
+    for (int j = 0; j < T::TN; ++j) {
+      const int n = n0 + (wn * T::TN + j) * 16 + (lane & 15);
+      if (n >= all_n) continue;
       f32x4 v = acc[i][j];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = v[e] * unit * scale;
-      if (p.kind == 1) {
-        uint16_t* o = static_cast<uint16_t*>(p.out) + at;
-        if (whole && ((uintptr_t)p.out & 7) == 0) {
-          *reinterpret_cast<ushort4*>(o) = make_ushort4(bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3]));
+      if constexpr (FOUR) {
+        const long at = base + (long)n * p.width + m;
+        if (p.kind == 1) {
+          *reinterpret_cast<ushort4*>(static_cast<uint16_t*>(p.out) + at) =
+              make_ushort4(bf16_bits(v[0]), bf16_bits(v[1]), bf16_bits(v[2]), bf16_bits(v[3]));
         } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + e < p.m) o[e] = bf16_bits(v[e]);
+          f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at);
+          if (p.kind == 3) v += *o;
+          *o = v;
         }
       } else {
-        float* o = static_cast<float*>(p.out) + at;
-        if (whole && ((uintptr_t)p.out & 15) == 0) {
-          if (p.kind == 3) v += *reinterpret_cast<const f32x4*>(o);
-          *reinterpret_cast<f32x4*>(o) = v;
-        } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + e < p.m) o[e] = p.kind == 3 ? o[e] + v[e] : v[e];
+        for (int e = 0; e < 4; ++e) {
+          if (m + e >= all_m) continue;
+          const long at = base + (long)(m + e) * p.width + n;
+          if (p.kind == 1) static_cast<uint16_t*>(p.out)[at] = bf16_bits(v[e]);
+          else if (p.kind == 3) static_cast<float*>(p.out)[at] += v[e];
+          else static_cast<float*>(p.out)[at] = v[e];
         }
       }
     }
   }
+}
+template <class T, bool FOUR>
+__global__ __launch_bounds__(T::THREADS) void k_loss_product(Product p) {
+  __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+  make_product<T, FOUR>(p, blockIdx.x, gridDim.x, blockIdx.y, lds);
+}
+// dh and dW of a piece in one launch, where both have few tiles: the first `first` work groups have dh's
+// tiles and ranges.
+template <class H, class W>
+__global__ __launch_bounds__(H::THREADS) void k_loss_products(Product h, Product w, int first, int tiles_h) {
+  static_assert(H::THREADS == W::THREADS);
+  __shared__ __attribute__((aligned(1024))) char lds[H::LDS > W::LDS ? H::LDS : W::LDS];
+  const int b = blockIdx.x;
+  if (b < first) make_product<H, false>(h, b % tiles_h, tiles_h, b / tiles_h, lds);
+  else make_product<W, false>(w, b - first, gridDim.x - first, 0, lds);
 }
 
 // Last kernel of the backward pass: sums of the ranges of k -> dh (the first `first` work groups), and
@@ -580,10 +609,13 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
     with_tile<NP, false, false>(side_along(q.count, a.rows, l.dp), [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
-      wino_launch((k_loss_logits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, part, best, hit);
-      part += tm;
+      const bool all = tm == 1 && q.count == a.classes;
+      wino_launch((k_loss_logits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, part, best, hit,
+                  all ? loss : nullptr, lse);
+      part += all ? 0 : tm;
     });
   }
+  if (part == 0) return hipGetLastError();
   // few rows: all threads of a work group on one
   if (a.rows >= 1024)
     wino_launch((k_loss_join<16>), dim3((a.rows + 15) / 16), dim3(256), st, (const float2*)best, part, (const float*)hit,
@@ -602,7 +634,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
   Numbers* num = reinterpret_cast<Numbers*>(ws + l.numbers);
   const float* ref = &num->ref;
   const Rows g{target, a.ignore_index, a.rows, a.classes};
-  wino_launch(k_loss_range, dim3(NP == 2 ? kRange : 1), dim3(256), st, NP == 2 ? (const float*)w : nullptr, a.w_stride,
+  wino_launch(k_loss_range, dim3(NP == 2 ? kRange : 1), dim3(1024), st, NP == 2 ? (const float*)w : nullptr, a.w_stride,
               NP == 2 ? (const float*)h : nullptr, a.h_stride, a.features, g, dloss, num);
   const bool w_direct = direct(a, w, a.w_stride);
   bool h_ready = false;   // always a copy: rows that are left out as zeros
@@ -627,25 +659,36 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
                   db);
     });
     const Operand od{dl, (long)vp * NP, 0, a.rows, vp};
-    if (dh) {
-      const int per = (int)up((vp + l.splits - 1) / l.splits, 64);
-      Product p{one ? dh : (void*)sums, a.features, (long)a.rows * a.features, one ? a.bf16 : first ? 3 : 2, vp, per,
-                a.features, a.rows, ref, &num->of_w};
-      with_tile<NP, true, false>(l.dh_side, [&](auto tile) {
+    const int per = (int)up((vp + l.splits - 1) / l.splits, 64), tk = (int)up(a.rows, 64);
+    const Product ph{od, ow, one ? dh : (void*)sums, (long)a.rows * a.features, one ? a.bf16 : first ? 3 : 2, vp, per,
+                     a.rows, a.features, ref, &num->of_w};
+    const Product pw{od, oh, dw ? const_cast<void*>(row_at(a, dw, first, a.features)) : nullptr, 0, a.bf16, tk, tk,
+                     q.count, a.features, ref, &num->of_h};
+    const int dw_side = side_for(q.count, a.features, 1);
+    const auto tiles = [](const Product& p, int side) { return (int)count_of(p.count, p.width, side); };
+    if (dh && dw && l.dh_side == 64 && dw_side == 64) {
+      typedef typename Tiles<NP, false, true>::Small H;
+      typedef typename Tiles<NP, true, true>::Small W;
+      const int th = tiles(ph, 64), all = th * l.splits;
+      wino_launch((k_loss_products<H, W>), dim3(all + tiles(pw, 64)), dim3(H::THREADS), st, ph, pw, all, th);
+    } else {
+      // tiles of 64 as in the launch of both, so that a gradient's bits do not go by which others are asked for
+      const auto whole = [&](const Product& p, int side) {
+        return side > 64 && a.features % 4 == 0 && ((uintptr_t)p.out & (p.kind == 1 ? 7 : 15)) == 0;
+      };
+      const auto launch = [&](auto tile, auto four, const Product& p, int ranges) {
         typedef decltype(tile) T;
-        const int tm = (a.features + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
-        wino_launch((k_loss_product<T>), dim3(tm * tn, l.splits), dim3(T::THREADS), st, ow, od, p, tm, tn);
-      });
-    }
-    if (dw) {
-      const int tk = (int)up(a.rows, 64);
-      Product p{const_cast<void*>(row_at(a, dw, first, a.features)), a.features, 0, a.bf16, tk, tk, a.features, q.count,
-                ref, &num->of_h};
-      with_tile<NP, true, true>(side_for(a.features, q.count, 1), [&](auto tile) {
-        typedef decltype(tile) T;
-        const int tm = (a.features + T::BM - 1) / T::BM, tn = (q.count + T::BN - 1) / T::BN;
-        wino_launch((k_loss_product<T>), dim3(tm * tn), dim3(T::THREADS), st, oh, od, p, tm, tn);
-      });
+        wino_launch((k_loss_product<T, decltype(four)::value>), dim3(tiles(p, T::BM), ranges), dim3(T::THREADS), st, p);
+      };
+      if (dh && whole(ph, l.dh_side))
+        with_tile<NP, true, false>(l.dh_side, [&](auto t) { launch(t, std::true_type{}, ph, l.splits); });
+      else if (dh)
+        with_tile<NP, false, true>(l.dh_side, [&](auto t) { launch(t, std::false_type{}, ph, l.splits); });
+      if (dw)
+        with_tile<NP, true, true>(dw_side, [&](auto t) {
+          if (whole(pw, dw_side)) launch(t, std::true_type{}, pw, 1);
+          else launch(t, std::false_type{}, pw, 1);
+        });
     }
   }
   const long items = (long)a.rows * a.features;
@@ -696,8 +739,7 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
       const long tiles = count_of((long)D, (long)T, side), slots = side == 256 ? 256 : 512;
       long ranges = slots / tiles;
       ranges = ranges > room ? room : ranges < 1 ? 1 : ranges;
-      const double rate = side == 256 ? 1.0 : side == 128 ? 0.93 : 0.85;
-      const double score = rate * D * T * ranges / ((double)((tiles * ranges + 255) / 256) * 256 * side * side);
+      const double score = rate_of(side) * D * T * ranges / ((double)((tiles * ranges + 255) / 256) * 256 * side * side);
       if (score > most) most = score, l.dh_side = side, l.splits = (int)ranges;
     }
     l.dh = take(4 * T * D * l.splits);

@@ -86,17 +86,20 @@ __device__ __forceinline__ f32x4 multiply_block(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Share of the 256 x 256 tiles' rate that other tiles reach when nothing is idle (16384 x 2048 x 4096 in bf16:
+// 1421 TFLOP/s and 1297; two planes, 13824 x 512 x 512: 128 x 128 tiles 22.2 us with 0.84 of the chip at work,
+// 64 x 64 ones 25.6 us with 0.96).
+inline double rate_of(int side) { return side == 256 ? 1.0 : side == 128 ? 0.92 : 0.8; }
 // Side of the square tiles (256, 128 or 64) for `z` products of m x n: the one that leaves least of the
-// chip idle, counting what of its tiles lies outside, compute units that wait for the others' last tile, and
-// the rates that tiles reach when nothing is idle (of the 256 x 256 ones; 10112 x 1024 x 576 and 16384 x 2048
-// x 4096: 1421, 1297 and about 1200 TFLOP/s).
+// chip idle, counting what of its tiles lies outside, and compute units that wait for the others' last tile.
+// (X of 6144 x 1536, k of 1536: 128 x 128 tiles 130 us, 64 x 64 ones 123; of 3 x 4608 x 512, k of 512: 33.5
+// and 39.)
 inline int side_for(double m, double n, double z) {
   int best = 64;
   double most = 0;
   for (int side = 256; side >= 64; side /= 2) {
     const double tiles = __builtin_ceil(m / side) * __builtin_ceil(n / side) * z;
-    const double rate = side == 256 ? 1.0 : side == 128 ? 0.93 : 0.85;
-    const double score = rate * m * n * z / (__builtin_ceil(tiles / 256) * 256 * side * side);
+    const double score = rate_of(side) * m * n * z / (__builtin_ceil(tiles / 256) * 256 * side * side);
     if (score > most) most = score, best = side;
   }
   return best;
@@ -239,7 +242,6 @@ struct Side {
 };
 #endif
 
-#if defined(__HIP_DEVICE_COMPILE__)
 // Two planes: upper and lower, lower and upper, upper and upper; one: its two parts of 32 k each.
 template <int NP, int TM, int TN>
 __device__ __forceinline__ void multiply_parts(const u32x4 (&a)[2][TM], const u32x4 (&b)[2][TN], f32x4 (&acc)[TM][TN]) {
@@ -253,6 +255,7 @@ __device__ __forceinline__ void multiply_parts(const u32x4 (&a)[2][TM], const u3
   }
 }
 
+#if defined(__HIP_DEVICE_COMPILE__)
 template <class T>
 __device__ __forceinline__ void multiply_few(const Operand& a, const Operand& b, long batch, int m0, int n0,
                                              int k_begin, int k_end, char* lds, f32x4& out) {

@@ -29,7 +29,7 @@ __device__ __forceinline__ float value(const void* p, long i, int bf16) {
 
 // Sums of squares of a matrix in 64 bits: no square over- or underflows.
 __global__ __launch_bounds__(256) void k_update_norm(const void* __restrict__ g, UpdateArgs a,
-                                                     double* __restrict__ norms) {
+                                                      double* __restrict__ norms) {
   __shared__ double lds[4];
   const long base = blockIdx.y * a.g_batch;
   double s = 0;
@@ -228,22 +228,21 @@ __global__ __launch_bounds__(T::THREADS) void k_update_product(Operand x, Operan
   }
 }
 
-// Sums of the ranges of a symmetric product's k, tiles of 64 x 64.
+// Sums of the ranges of a symmetric product's k, 32 x 32 a work group.
 template <Kind KIND>
 __global__ __launch_bounds__(256) void k_update_join(const float* __restrict__ parts, int count, long part,
                                                      int part_ld, Result s) {
   int tm, tn;
   triangle(blockIdx.x, tm, tn);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = tn * 64 + wave * 16 + (lane & 15), m = tm * 64 + i * 16 + (lane >> 4) * 4;
-    f32x4 v = {0, 0, 0, 0};
-    if (n < s.r && m < part_ld)
-      for (int q = 0; q < count; ++q)
-        v += *reinterpret_cast<const f32x4*>(parts + q * part + ((long)blockIdx.z * s.r + n) * part_ld + m);
-    finish<KIND>(s, blockIdx.z, m, n, v, tm != tn);
+  const int n = tn * 32 + (wave >> 1) * 16 + (lane & 15), m = tm * 32 + (wave & 1) * 16 + (lane >> 4) * 4;
+  f32x4 v = {0, 0, 0, 0};
+  if (n < s.r) {
+    const float* from = parts + ((long)blockIdx.y * s.r + n) * part_ld + m;
+#pragma unroll 4
+    for (int q = 0; q < count; ++q) v += *reinterpret_cast<const f32x4*>(from + q * part);
   }
+  finish<KIND>(s, blockIdx.y, m, n, v, tm != tn);
 }
 
 // The symmetric products of few rows.
@@ -268,13 +267,14 @@ struct Tiles {
   typedef Tile<256, 256, 2, 4, 2, 2, AX> Big;
   typedef Tile<128, 128, 2, 2, 2, 2, AX> Mid;
   typedef Tile<64, 64, 2, 2, 2, 2, AX> Small;
+  typedef Tile<64, 64, 2, 2, 2, 4, AX> Deep;   // where two work groups a compute unit are all there are
 };
 
 int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
 int half_of(int tiles) { return tiles * (tiles + 1) / 2; }
 
-// Symmetric products of few tiles and not many k: no barriers, one launch.  (3 matrices of 256 rows, k of
-// 2304: 20.9 us, against ? in ranges with a join.)
+// Symmetric products of few tiles and not many k: no barriers, one launch.  (A of 4 x 64 rows, k of 576: 8.4
+// us, and 9.5 in four ranges with their join; of 3 x 256 rows, k of 2304: 20.9 us and 18.9.)
 bool few(const UpdateLayout& l, int batch, int k) { return (long)l.r * l.r * batch <= 256L * 256 * 4 && k <= 1024; }
 
 template <Kind KIND>
@@ -297,10 +297,11 @@ void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& 
       wino_launch((k_update_product<T, KIND>), dim3(tiles * batch, splits), dim3(T::THREADS), st, x, y, k, per,
                   tiles, 0, s, splits > 1 ? parts : nullptr, part, l.rp);
       if (splits > 1)
-        wino_launch((k_update_join<KIND>), dim3(half_of(tiles_of(l.rp, 64)), 1, batch), dim3(256), st,
+        wino_launch((k_update_join<KIND>), dim3(half_of(tiles_of(l.rp, 32)), batch), dim3(256), st,
                     (const float*)parts, splits, part, l.rp, s);
     };
     if (l.side == 128 && KIND == kGram) go(Tiles<false>::Mid{});
+    else if ((long)half_of(tiles_of(l.r, 64)) * batch * (KIND == kGram ? l.splits : 1) <= 512) go(Tiles<false>::Deep{});
     else go(Tiles<false>::Small{});
   } else {
     const auto go = [&](auto tile) {
@@ -312,6 +313,7 @@ void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& 
     const int side = side_for(l.c, l.r, batch);
     if (side == 256) go(Tiles<true>::Big{});
     else if (side == 128) go(Tiles<true>::Mid{});
+    else if ((long)tiles_of(l.c, 64) * tiles_of(l.r, 64) * batch <= 512) go(Tiles<true>::Deep{});
     else go(Tiles<true>::Small{});
   }
 }
