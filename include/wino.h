@@ -464,8 +464,8 @@ int wino_linear_cross_entropy(const wino_loss_desc_t* d, const void* h, const vo
  *   dh = dl w,  dw = dl^T h,  dbias = sum_t dl
  * dh [rows][features] and dw [classes][features] dense, of `type`; dbias
  * [classes] fp32; each may be null.  Before the two products dl / max|dloss| is
- * rounded, for bf16 to bf16, for fp32 like the other factors (dbias sums it
- * unrounded).  Without rows dw and dbias
+ * rounded, for bf16 to bf16 (for 64 rows or fewer, and small products, to 16
+ * bits), for fp32 like the other factors (dbias sums it unrounded).  Without rows dw and dbias
  * are zeros. */
 int wino_linear_cross_entropy_backward_workspace_bytes(const wino_loss_desc_t* d, size_t* bytes);
 int wino_linear_cross_entropy_backward(const wino_loss_desc_t* d, const void* h, const void* w,

@@ -10,7 +10,9 @@
 // (wino_products.hpp), so none of them is transposed in memory.
 //
 // bf16 operands are taken where they lie if their rows are whole pieces of 16 bytes and whole lines, and
-// from a padded copy otherwise; dl is rounded to bf16 like the gradients.  fp32 operands become two
+// from a padded copy otherwise; dl is rounded to bf16 like the gradients (of few rows, whose roundings do
+// not average out, or small products to two bf16 values: one row of two classes was off by 0.004 of the
+// gradient, twice a bf16 result's rounding).  fp32 operands become two
 // fp16 planes (22 bits) under one power of two for W and one for h (in the forward pass one a row, so that
 // no row's magnitude touches another's lse); in the backward pass rows that are left out count as
 // zeros, whatever they hold, and do not enter the power of two.  dl is kept relative to the largest
@@ -338,13 +340,15 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* __restrict__ be
   finish_row(g, t, top, lds[1][0][x], hit, loss, lse);
 }
 
-// Backward: dl / ref of a piece, rows [t][ld]; the sums over a wave's rows for dbias.
+// Backward: dl / ref of a piece, rows [t][ld]; `rest`, may be null: what bf16 leaves of it; the sums over a
+// wave's rows for dbias.
 template <class T>
 __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand h, Logits g, int tiles_m,
                                                              int tiles_n, const float* __restrict__ lse,
                                                              const float* __restrict__ dloss,
                                                              const float* __restrict__ ref,
                                                              uint16_t* __restrict__ dl, int ld,
+                                                             uint16_t* __restrict__ rest,
                                                              float* __restrict__ dbias) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   int tm, tn;
@@ -389,11 +393,17 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
         for (int p = 0; p < T::NP; ++p)
           *reinterpret_cast<ushort4*>(dl + (long)t * ld * T::NP + place<T::NP>(v) + p * 32) =
               make_ushort4(out[0][p], out[1][p], out[2][p], out[3][p]);
+        if (T::NP == 1 && rest)
+          *reinterpret_cast<ushort4*>(rest + (long)t * ld + v) =
+              make_ushort4(bf16_bits(d[0] - bf16_value(out[0][0])), bf16_bits(d[1] - bf16_value(out[1][0])),
+                           bf16_bits(d[2] - bf16_value(out[2][0])), bf16_bits(d[3] - bf16_value(out[3][0])));
         // tiles of 32 end where the line's last ones have no rows of W: zeros behind them
         if (is_few<T> && tm + 1 == tiles_m && v + 32 < ld)
 #pragma unroll
           for (int p = 0; p < T::NP; ++p)
             *reinterpret_cast<ushort4*>(dl + (long)t * ld * T::NP + place<T::NP>(v + 32) + p * 32) = make_ushort4(0, 0, 0, 0);
+        if (is_few<T> && T::NP == 1 && rest && tm + 1 == tiles_m && v + 32 < ld)
+          *reinterpret_cast<ushort4*>(rest + (long)t * ld + v + 32) = make_ushort4(0, 0, 0, 0);
       }
     }
   }
@@ -420,6 +430,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
 // 640; of 10007 x 515 in fp32, whose rows start anywhere: 60 and 55.)
 struct Product {
   Operand rows, features;
+  const uint16_t* rest;  // of `rows`, may be null: a second product on top of the first
   void* out;
   long split;            // elements between ranges of k
   int kind, k, per;      // k in all and per range
@@ -436,6 +447,12 @@ __device__ __forceinline__ void make_product(const Product& p, int group, int gr
   const int m0 = tm * T::BM, n0 = tn * T::BN;
   f32x4 acc[T::TM][T::TN] = {};
   const int k0 = range * p.per, k1 = k0 + p.per < p.k ? k0 + p.per : p.k;
+  if (T::NP == 1 && p.rest) {   // the smaller one first
+    Operand rest = p.rows;
+    rest.p = p.rest;
+    multiply<T>(FOUR ? a : rest, FOUR ? rest : b, 0, m0, n0, k0, k1, lds, acc);
+    __syncthreads();
+  }
   multiply<T>(a, b, 0, m0, n0, k0, k1, lds, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
@@ -641,6 +658,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
   Operand oh{}, ow{};
   Logits q{bias, g, 0, 0, l.dp, &num->of_w, &num->of_h, 0};
   uint16_t* dl = reinterpret_cast<uint16_t*>(ws + l.dl);
+  uint16_t* rest = l.two ? reinterpret_cast<uint16_t*>(ws + l.rest) : nullptr;
   float* db = dbias ? reinterpret_cast<float*>(ws + l.dbias) : nullptr;
   float* sums = reinterpret_cast<float*>(ws + l.dh);
   const bool one = l.splits == 1 && l.piece >= a.classes;   // dh comes from one product
@@ -656,13 +674,13 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
       parts = tn * T::WN;
       wino_launch((k_loss_dlogits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, lse, dloss, ref, dl, vp,
-                  db);
+                  rest, db);
     });
     const Operand od{dl, (long)vp * NP, 0, a.rows, vp};
     const int per = (int)up((vp + l.splits - 1) / l.splits, 64), tk = (int)up(a.rows, 64);
-    const Product ph{od, ow, one ? dh : (void*)sums, (long)a.rows * a.features, one ? a.bf16 : first ? 3 : 2, vp, per,
+    const Product ph{od, ow, rest, one ? dh : (void*)sums, (long)a.rows * a.features, one ? a.bf16 : first ? 3 : 2, vp, per,
                      a.rows, a.features, ref, &num->of_w};
-    const Product pw{od, oh, dw ? const_cast<void*>(row_at(a, dw, first, a.features)) : nullptr, 0, a.bf16, tk, tk,
+    const Product pw{od, oh, rest, dw ? const_cast<void*>(row_at(a, dw, first, a.features)) : nullptr, 0, a.bf16, tk, tk,
                      q.count, a.features, ref, &num->of_h};
     const int dw_side = side_for(q.count, a.features, 1);
     const auto tiles = [](const Product& p, int side) { return (int)count_of(p.count, p.width, side); };
@@ -730,6 +748,10 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
     l.unit_h = take(4 * T);
   } else {
     l.dl = take(item * T * vp);
+    // bf16: dl's rounding averages out over many rows; with few of them, or little to do, it is kept on
+    // two bf16 values
+    l.two = a.bf16 && (T <= 64 || (double)T * D * V <= 1 << 30);
+    if (l.two) l.rest = take(item * T * vp);
     l.side = side_along((long)P, (long)T, l.dp);
     // ranges of classes, each of 512 or more, until dh's tiles fill the chip: one tile of 256 a compute
     // unit, or two of the smaller ones
