@@ -500,17 +500,18 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_product(Product p) {
   make_product<T, FOUR>(p, blockIdx.x, gridDim.x, blockIdx.y, lds);
 }
 // dh and dW of a piece in one launch, where both have few tiles: the first `first` work groups have dh's
-// tiles and ranges.
+// tiles and ranges, the others dW's.
 template <class H, class W>
-__global__ __launch_bounds__(H::THREADS) void k_loss_products(Product h, Product w, int first, int tiles_h) {
+__global__ __launch_bounds__(H::THREADS) void k_loss_products(Product h, Product w, int first, int tiles_h,
+                                                              int tiles_w) {
   static_assert(H::THREADS == W::THREADS);
   __shared__ __attribute__((aligned(1024))) char lds[H::LDS > W::LDS ? H::LDS : W::LDS];
   const int b = blockIdx.x;
   if (b < first) make_product<H, false>(h, b % tiles_h, tiles_h, b / tiles_h, lds);
-  else make_product<W, false>(w, b - first, gridDim.x - first, 0, lds);
+  else make_product<W, false>(w, (b - first) % tiles_w, tiles_w, (b - first) / tiles_w, lds);
 }
 
-// Last kernel of the backward pass: sums of the ranges of k -> dh (the first `first` work groups), and
+// Sums of the ranges of k -> dh or dW (the first `first` work groups), and, as the backward pass's last kernel,
 // of the waves' rows -> dbias.
 __global__ __launch_bounds__(256) void k_loss_sums(const float* __restrict__ sums, int count, long items, int bf16,
                                                    void* __restrict__ out, unsigned first,
@@ -520,6 +521,7 @@ __global__ __launch_bounds__(256) void k_loss_sums(const float* __restrict__ sum
   if (blockIdx.x < first) {
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long)first * 256) {
       float s = 0;
+#pragma unroll 8
       for (int q = 0; q < count; ++q) s += sums[q * items + i];
       s *= scale;
       if (bf16) static_cast<uint16_t*>(out)[i] = bf16_bits(s);
@@ -552,7 +554,9 @@ struct Tiles {
   typedef Tile<256, 256, 2, 4, NP, 2, AX, BX> Big;
   typedef Tile<128, 128, 2, 2, NP, 2, AX, BX> Mid;
   typedef Tile<64, 64, 2, 2, NP, 2, AX, BX> Small;
+  typedef Tile<64, 64, 2, 2, NP, 4, AX, BX> Deep;   // where two work groups a compute unit are all there are
 };
+constexpr long kDeepGroups = 512;
 long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
 // The same of products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the
 // waves where there are few tiles.
@@ -563,10 +567,11 @@ int side_along(long m, long n, long k) {
 constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
 
 template <int NP, bool AX, bool BX, class F>
-void with_tile(int side, F&& f) {
+void with_tile(int side, long groups, F&& f) {
   if (side == 256) f(typename Tiles<NP, AX, BX>::Big{});
   else if (side == 32 && !AX && !BX) f(Few<NP>{});
   else if (side == 128) f(typename Tiles<NP, AX, BX>::Mid{});
+  else if (groups <= kDeepGroups) f(typename Tiles<NP, AX, BX>::Deep{});
   else f(typename Tiles<NP, AX, BX>::Small{});
 }
 
@@ -623,7 +628,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
     q.count = (int)(a.classes - first < piece ? a.classes - first : piece);
     operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, num, ws, &ow, &oh, st);
     h_ready = true;
-    with_tile<NP, false, false>(side_along(q.count, a.rows, l.dp), [&](auto tile) {
+    with_tile<NP, false, false>(side_along(q.count, a.rows, l.dp), count_of(q.count, a.rows, 64), [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
       const bool all = tm == 1 && q.count == a.classes;
@@ -669,7 +674,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
     const int vp = (int)up(q.count, 64);
     operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, true, num, ws, &ow, &oh, st);
     h_ready = true;
-    with_tile<NP, false, false>(l.side, [&](auto tile) {
+    with_tile<NP, false, false>(l.side, count_of(q.count, a.rows, 64), [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
       parts = tn * T::WN;
@@ -678,17 +683,27 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
     });
     const Operand od{dl, (long)vp * NP, 0, a.rows, vp};
     const int per = (int)up((vp + l.splits - 1) / l.splits, 64), tk = (int)up(a.rows, 64);
+    const int dw_per = (int)up((tk + l.dw_splits - 1) / l.dw_splits, 64);
+    float* dw_sums = l.dw_splits > 1 ? reinterpret_cast<float*>(ws + l.dw) : nullptr;
+    void* dw_rows = dw ? const_cast<void*>(row_at(a, dw, first, a.features)) : nullptr;
+    const long dw_items = (long)q.count * a.features;
     const Product ph{od, ow, rest, one ? dh : (void*)sums, (long)a.rows * a.features, one ? a.bf16 : first ? 3 : 2, vp, per,
                      a.rows, a.features, ref, &num->of_w};
-    const Product pw{od, oh, rest, dw ? const_cast<void*>(row_at(a, dw, first, a.features)) : nullptr, 0, a.bf16, tk, tk,
-                     q.count, a.features, ref, &num->of_h};
-    const int dw_side = side_for(q.count, a.features, 1);
+    const Product pw{od, oh, rest, dw_sums ? (void*)dw_sums : dw_rows, dw_items, dw_sums ? 2 : a.bf16, tk, dw_per, q.count,
+                     a.features, ref, &num->of_h};
+    const int dw_side = dw_sums ? 64 : side_for(q.count, a.features, 1);
     const auto tiles = [](const Product& p, int side) { return (int)count_of(p.count, p.width, side); };
     if (dh && dw && l.dh_side == 64 && dw_side == 64) {
-      typedef typename Tiles<NP, false, true>::Small H;
-      typedef typename Tiles<NP, true, true>::Small W;
-      const int th = tiles(ph, 64), all = th * l.splits;
-      wino_launch((k_loss_products<H, W>), dim3(all + tiles(pw, 64)), dim3(H::THREADS), st, ph, pw, all, th);
+      const int th = tiles(ph, 64), tw = tiles(pw, 64), all = th * l.splits;
+      const auto launch = [&](auto h, auto w) {
+        typedef decltype(h) H;
+        typedef decltype(w) W;
+        wino_launch((k_loss_products<H, W>), dim3(all + tw * l.dw_splits), dim3(H::THREADS), st, ph, pw, all, th, tw);
+      };
+      if (all + tw * l.dw_splits <= kDeepGroups)
+        launch(typename Tiles<NP, false, true>::Deep{}, typename Tiles<NP, true, true>::Deep{});
+      else
+        launch(typename Tiles<NP, false, true>::Small{}, typename Tiles<NP, true, true>::Small{});
     } else {
       // tiles of 64 as in the launch of both, so that a gradient's bits do not go by which others are asked for
       const auto whole = [&](const Product& p, int side) {
@@ -698,15 +713,21 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
         typedef decltype(tile) T;
         wino_launch((k_loss_product<T, decltype(four)::value>), dim3(tiles(p, T::BM), ranges), dim3(T::THREADS), st, p);
       };
+      const long groups_h = (long)tiles(ph, 64) * l.splits, groups_w = (long)tiles(pw, 64) * l.dw_splits;
       if (dh && whole(ph, l.dh_side))
-        with_tile<NP, true, false>(l.dh_side, [&](auto t) { launch(t, std::true_type{}, ph, l.splits); });
+        with_tile<NP, true, false>(l.dh_side, groups_h, [&](auto t) { launch(t, std::true_type{}, ph, l.splits); });
       else if (dh)
-        with_tile<NP, false, true>(l.dh_side, [&](auto t) { launch(t, std::false_type{}, ph, l.splits); });
+        with_tile<NP, false, true>(l.dh_side, groups_h, [&](auto t) { launch(t, std::false_type{}, ph, l.splits); });
       if (dw)
-        with_tile<NP, true, true>(dw_side, [&](auto t) {
-          if (whole(pw, dw_side)) launch(t, std::true_type{}, pw, 1);
-          else launch(t, std::false_type{}, pw, 1);
+        with_tile<NP, true, true>(dw_side, groups_w, [&](auto t) {
+          if (whole(pw, dw_side)) launch(t, std::true_type{}, pw, l.dw_splits);
+          else launch(t, std::false_type{}, pw, l.dw_splits);
         });
+    }
+    if (dw && dw_sums) {
+      const unsigned grid = grid_of(dw_items, 8192);
+      wino_launch(k_loss_sums, dim3(grid), dim3(256), st, (const float*)dw_sums, l.dw_splits, dw_items, a.bf16, dw_rows, grid,
+                  (const float*)nullptr, 0, 0, (float*)nullptr, ref);
     }
   }
   const long items = (long)a.rows * a.features;
@@ -764,7 +785,14 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
       const double score = rate_of(side) * D * T * ranges / ((double)((tiles * ranges + 255) / 256) * 256 * side * side);
       if (score > most) most = score, l.dh_side = side, l.splits = (int)ranges;
     }
+    if (l.splits > 64) l.splits = 64;   // k_loss_sums adds them up one after the other
     l.dh = take(4 * T * D * l.splits);
+    // ranges of rows, each of 256 or more, where dW has few tiles of 64
+    const long tiles = count_of((long)P, (long)D, 64);
+    long ranges = tiles < 128 ? 256 / tiles : 1;
+    if (ranges > (long)T / 256) ranges = (long)T / 256;
+    l.dw_splits = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
+    if (l.dw_splits > 1) l.dw = take(4 * P * D * l.dw_splits);
     l.dbias = take(4 * V * waves_n(l.side) * (T ? (T + l.side - 1) / l.side : 1));
   }
   l.bytes = at;

@@ -39,8 +39,9 @@ struct LossLayout {
   int piece, dp;          // classes per piece; features rounded up to whole lines
   int side, dh_side;      // tiles of dl's and dh's products
   int splits;             // ranges of the classes of a piece in dh's product
+  int dw_splits;          // ranges of the rows in dW's product
   int two;                // bf16: dl on two values
-  size_t numbers, w, h, parts, target, unit_w, unit_h, dl, rest, dh, dbias, bytes;
+  size_t numbers, w, h, parts, target, unit_w, unit_h, dl, rest, dh, dw, dbias, bytes;
 };
 LossLayout loss_layout(const LossArgs& a, bool backward);
 hipError_t launch_loss(const LossArgs& a, const void* h, const void* w, const float* bias,
