@@ -1,0 +1,281 @@
+"""The training operators as a program uses them: a step of a small network through the layers and the
+operators, captured and replayed calls, calls on two streams at once, tensors past 32-bit offsets.
+
+Every stage of the network's step is held to the oracle's on the stage's own inputs; the tolerances are
+those derived in the operators' and the backward pass's own tests, as the largest difference over the
+largest reference value: fp32 sums of at most 300 terms and factors of 22 bits, 1e-5.
+"""
+import numpy as np
+import pytest
+
+from helpers import small_layer
+from oracle import backward as bw
+from oracle import training as tr
+
+pytestmark = pytest.mark.gpu
+
+
+def near(got, ref, tol=1e-5):
+    got = got.double().cpu().numpy()
+    assert got.shape == ref.shape
+    assert np.abs(got - ref).max() <= tol * np.abs(ref).max()
+
+
+def test_a_networks_step():
+    """Two layers with a norm between them (int8 codes out), a classifier of every pixel behind them: loss,
+    gradients back through everything, updates."""
+    import torch
+    import paper_2004_11077_amd as wn
+    dev = torch.device("cuda:0")
+    N, H, W, C, classes, m = 2, 8, 8, 32, 37, 4
+    xq, wq, s_x, s_w = small_layer(N, H, W, C, C, seed=11)
+    w2q = small_layer(N, H, W, C, C, seed=12)[1]
+    rng = np.random.default_rng(3)
+    desc = wn.ConvDesc(N, H, W, C, C, m=m)
+    n2, T, rows = desc.n ** 2, desc.tiles, N * H * W
+    cuda = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(dev)
+    new = lambda *s, dtype=torch.float32: torch.full(s, 7, dtype=dtype, device=dev)
+    room = lambda n: torch.empty(n, dtype=torch.uint8, device=dev)
+    cws = room(wn.wino_calibrate_workspace_bytes(desc))
+
+    def layer(x, w, s_in):
+        sc = wn.wino_calibrate(desc, x, w, None, float(s_in), float(s_w), cws)
+        U, V = new(n2, T, C, dtype=torch.int8), new(n2, C, C, dtype=torch.int8)
+        M, y = new(n2, T, C, dtype=torch.int8), new(N, H, W, C)
+        wn.wino_transform_operands(desc, x, U, w, V, sc)
+        wn.wino_contract(desc, U, V, M, sc)
+        wn.wino_output_transform(desc, M, y, sc)
+        return sc, U, V, y
+
+    x1, w1, w2 = cuda(xq), cuda(wq), cuda(w2q)
+    gamma = cuda((1 + 0.1 * rng.standard_normal(C)).astype(np.float32))
+    beta = cuda((0.1 * rng.standard_normal(C)).astype(np.float32))
+    wc = cuda((rng.standard_normal((classes, C)) / 6).astype(np.float32))
+    bias = cuda((0.1 * rng.standard_normal(classes)).astype(np.float32))
+    target = cuda(np.where(rng.random(rows) < 0.1, -100, rng.integers(0, classes, rows)))
+    s_y = 3.0 / 127
+    norm = wn.NormDesc(rows, C, y_type=wn.TYPE_I8, s_y=s_y)
+    loss_desc = wn.LossDesc(rows, C, classes)
+
+    # forward
+    sc1, U1, V1, y1 = layer(x1, w1, s_x)
+    x2, mean, rstd = new(N, H, W, C, dtype=torch.int8), new(rows), new(rows)
+    wn.wino_layer_norm(norm, y1, gamma, beta, x2, mean, rstd)
+    sc2, U2, V2, y2 = layer(x2, w2, s_y)
+    loss, lse = new(rows), new(rows)
+    ws = room(max(wn.wino_linear_cross_entropy_workspace_bytes(loss_desc), wn.wino_linear_cross_entropy_backward_workspace_bytes(loss_desc)))
+    wn.wino_linear_cross_entropy(loss_desc, y2, wc, bias, target, loss, lse, ws)
+
+    # backward
+    dloss = (target >= 0).float() / (target >= 0).sum()
+    dy2, dwc, dbias = new(N, H, W, C), new(classes, C), new(classes)
+    wn.wino_linear_cross_entropy_backward(loss_desc, y2, wc, bias, target, lse, dloss, dy2, dwc, dbias, ws)
+    bws = room(wn.wino_backward_workspace_bytes(desc))
+    dx2, dw2, dx1, dw1 = new(N, H, W, C), new(C, C, 3, 3), new(N, H, W, C), new(C, C, 3, 3)
+    wn.wino_backward(desc, dy2, U2, V2, sc2, dx2, dw2, bws)
+    dy1, dgamma, dbeta = new(N, H, W, C), new(C), new(C)
+    nws = room(wn.wino_layer_norm_backward_workspace_bytes(norm))
+    wn.wino_layer_norm_backward(norm, dx2, y1, gamma, mean, rstd, dy1, dgamma, dbeta, nws)
+    wn.wino_backward(desc, dy1, U1, V1, sc1, dx1, dw1, bws)
+
+    # updates of both layers' filters at once
+    od = wn.OrthogonaliseDesc(2, C, 9 * C, scale=0.2)
+    g, o = torch.stack([dw1, dw2]), new(2, C, C, 3, 3)
+    wn.wino_orthogonalise(od, g, o, room(wn.wino_orthogonalise_workspace_bytes(od)))
+    torch.cuda.synchronize()
+
+    # stage by stage
+    d = lambda t: t.double().cpu().numpy()
+    flat = lambda t: d(t).reshape(rows, C)
+    eps = np.float64(np.float32(1e-5))
+    ref, rmean, rrstd = tr.layer_norm(flat(y1), d(gamma), d(beta), eps)
+    assert np.array_equal(flat(x2), tr.codes(ref, s_y).astype(np.float64))
+    near(mean, rmean)
+    near(rstd, rrstd)
+    t = target.cpu().numpy()
+    rloss, rlse = tr.cross_entropy(flat(y2), d(wc), d(bias), t)
+    near(loss, rloss)
+    near(lse, rlse)
+    rdh, rdw, rdb, _ = tr.cross_entropy_backward(flat(y2), d(wc), d(bias), t, d(dloss))
+    near(dy2.view(rows, C), rdh)
+    near(dwc, rdw)
+    near(dbias, rdb)
+    for dy, U, V, sc, dx, dw in ((dy2, U2, V2, sc2, dx2, dw2), (dy1, U1, V1, sc1, dx1, dw1)):
+        back = bw.backward_layer(d(dy), bw.dequantise(U.cpu().numpy(), sc.s_u), bw.dequantise(V.cpu().numpy(), sc.s_v), (N, H, W, C), m)
+        near(dx, back["dx"])
+        near(dw, back["dw"])
+    rdx, rdg, rdbeta = tr.layer_norm_backward(flat(dx2), flat(y1), d(gamma), d(mean), d(rstd))
+    near(dy1.view(rows, C), rdx)
+    near(dgamma, rdg)
+    near(dbeta, rdbeta)
+    for i, dw in enumerate((dw1, dw2)):
+        ref, _ = tr.orthogonalise(d(dw).reshape(C, 9 * C), scale=np.float64(np.float32(0.2)))
+        # 4^5 times the error of one product, 2^-22 of 10.3 times, over a largest value of a few sqrt(1 / 9 C)
+        assert np.linalg.norm(d(o[i]).reshape(C, 9 * C) - ref) <= 4 ** 5 * 10.3 * 4 * 2.0 ** -22 * np.linalg.norm(ref)
+
+
+def operators(seed):
+    """(name, call, outputs) of every operator on inputs of its own; a call takes its stream."""
+    import torch
+    import paper_2004_11077_amd as wn
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    r = lambda *s, dtype=torch.float32: torch.randn(*s, generator=g, device="cuda").to(dtype)
+    room = lambda n: torch.empty(n, dtype=torch.uint8, device="cuda")
+    all = []
+    for dtype, code in ((torch.float32, wn.TYPE_F32), (torch.bfloat16, wn.TYPE_BF16)):
+        rows, channels = 700, 96
+        nd = wn.NormDesc(rows, channels, x_type=code, y_type=code, g_type=code)
+        x, dy, gamma, beta = r(rows, channels, dtype=dtype), r(rows, channels, dtype=dtype), r(channels), r(channels)
+        y, dx, mean, rstd, dgamma, dbeta = torch.empty_like(x), torch.empty_like(x), r(rows), r(rows), r(channels), r(channels)
+        nws = room(wn.wino_layer_norm_backward_workspace_bytes(nd))
+
+        def norm(stream, nd=nd, x=x, dy=dy, gamma=gamma, beta=beta, y=y, dx=dx, mean=mean, rstd=rstd, dgamma=dgamma, dbeta=dbeta, nws=nws):
+            wn.wino_layer_norm(nd, x, gamma, beta, y, mean, rstd, stream)
+            wn.wino_layer_norm_backward(nd, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, nws, stream)
+        all.append(("norm", norm, [y, mean, rstd, dx, dgamma, dbeta], [x, dy], [nws]))
+
+        T, D, V = 300, 128, 3000
+        ld = wn.LossDesc(T, D, V, type=code, piece=1024)
+        h, w, bias = r(T, D, dtype=dtype), r(V, D, dtype=dtype), r(V)
+        target = torch.randint(-1, V, (T,), generator=g, device="cuda")
+        dloss, loss, lse, dbias = r(T), r(T), r(T), r(V)
+        dh, dw = torch.empty_like(h), torch.empty_like(w)
+        lws = room(max(wn.wino_linear_cross_entropy_workspace_bytes(ld), wn.wino_linear_cross_entropy_backward_workspace_bytes(ld)))
+
+        def entropy(stream, ld=ld, h=h, w=w, bias=bias, target=target, dloss=dloss, loss=loss, lse=lse, dbias=dbias, dh=dh, dw=dw, lws=lws):
+            wn.wino_linear_cross_entropy(ld, h, w, bias, target, loss, lse, lws, stream)
+            wn.wino_linear_cross_entropy_backward(ld, h, w, bias, target, lse, dloss, dh, dw, dbias, lws, stream)
+        all.append(("loss", entropy, [loss, lse, dh, dw, dbias], [h, w], [lws]))
+
+        od = wn.OrthogonaliseDesc(2, 96, 864, g_type=code, o_type=code)
+        grad = r(2, 96, 864, dtype=dtype)
+        o = torch.empty_like(grad)
+        ows = room(wn.wino_orthogonalise_workspace_bytes(od))
+
+        def update(stream, od=od, grad=grad, o=o, ows=ows):
+            wn.wino_orthogonalise(od, grad, o, ows, stream)
+        all.append(("update", update, [o], [grad], [ows]))
+    return all
+
+
+def test_captured_calls_replay_to_the_eager_results():
+    import torch
+    for name, call, outputs, inputs, spaces in operators(1):
+        s = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            call(s)
+            torch.cuda.synchronize()
+            eager = [t.clone() for t in outputs]
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                call(s)
+        for rep in range(4):
+            for t in outputs + spaces:
+                t.fill_(rep + 1)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outputs, eager)), (name, rep)
+        # other inputs through the same graph
+        for t in inputs:
+            t.copy_(t.flip(0))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outputs]
+        call(None)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outputs, got)), name
+        assert not all(torch.equal(a, b) for a, b in zip(got, eager)), name
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Replayed one after the other on one stream, as their owner orders them."""
+    import torch
+    import paper_2004_11077_amd as wn
+    sizes = [(40, 96), (64, 576)]
+    descs = [wn.OrthogonaliseDesc(1, *s) for s in sizes]
+    ws = torch.empty(max(wn.wino_orthogonalise_workspace_bytes(d) for d in descs), dtype=torch.uint8, device="cuda")
+    gs = [torch.randn(1, *s, device="cuda") for s in sizes]
+    os = [torch.empty_like(g) for g in gs]
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs, eager = [], []
+    with torch.cuda.stream(s):
+        for d, g, o in zip(descs, gs, os):
+            wn.wino_orthogonalise(d, g, o, ws, s)
+            torch.cuda.synchronize()
+            eager.append(o.clone())
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=s):
+                wn.wino_orthogonalise(d, g, o, ws, s)
+    for _ in range(3):
+        for o in os:
+            o.zero_()
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(os, eager))
+
+
+def test_calls_on_two_streams_at_once():
+    import torch
+    first, second = operators(2), operators(3)
+    expected = []
+    for _, call, outputs, _, _ in first + second:
+        call(None)
+        torch.cuda.synchronize()
+        expected.append([t.clone() for t in outputs])
+        for t in outputs:
+            t.zero_()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for x, y in zip(first, second):
+        x[1](a)
+        y[1](b)
+    torch.cuda.synchronize()
+    for (name, _, outputs, _, _), ref in zip(first + second, expected):
+        assert all(torch.equal(t, r) for t, r in zip(outputs, ref)), name
+
+
+def test_weights_and_gradients_past_32_bit_offsets():
+    import torch
+    import paper_2004_11077_amd as wn
+    T, D, V, stride = 5, 64, 70000, 65536                     # w spans 4.6e9 elements of bf16: 9.2 GB
+    whole = torch.empty(V * stride, dtype=torch.bfloat16, device="cuda")
+    w = whole.view(V, stride)[:, :D]
+    w.copy_(torch.randn(V, D, device="cuda") / 8)
+    dense = w.contiguous()
+    h = torch.randn(T, D, device="cuda").to(torch.bfloat16)
+    target = torch.tensor([0, V - 1, V // 2, -100, 40000], device="cuda")
+    dloss = torch.full((T,), 0.25, device="cuda")
+    results = []
+    for weights, s in ((w, stride), (dense, 0)):
+        desc = wn.LossDesc(T, D, V, type=wn.TYPE_BF16, w_stride=s)
+        ws = torch.empty(max(wn.wino_linear_cross_entropy_workspace_bytes(desc), wn.wino_linear_cross_entropy_backward_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+        loss, lse = torch.empty(2, T, device="cuda")
+        dh, dw = torch.empty_like(h), torch.empty_like(dense)
+        wn.wino_linear_cross_entropy(desc, h, weights, None, target, loss, lse, ws)
+        wn.wino_linear_cross_entropy_backward(desc, h, weights, None, target, lse, dloss, dh, dw, None, ws)
+        results.append((loss, lse, dh, dw))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    ref = tr.cross_entropy(h.double().cpu().numpy(), dense.double().cpu().numpy(), None, target.cpu().numpy())[0]
+    near(results[0][0], ref)
+
+
+def test_gradients_past_32_bit_offsets():
+    import torch
+    import paper_2004_11077_amd as wn
+    r, c, apart = 48, 100, (1 << 31) + 16                     # the second matrix starts 4.3 GB on
+    whole = torch.empty(apart + r * c, dtype=torch.bfloat16, device="cuda")
+    g = torch.as_strided(whole, (2, r, c), (apart, c, 1))
+    g.copy_(torch.randn(2, r, c, device="cuda"))
+    dense = g.contiguous()
+    out = [torch.empty(2, r, c, device="cuda") for _ in range(2)]
+    for t, o, b in ((g, out[0], apart), (dense, out[1], 0)):
+        desc = wn.OrthogonaliseDesc(2, r, c, g_type=wn.TYPE_BF16, g_batch=b)
+        ws = torch.empty(wn.wino_orthogonalise_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+        wn.wino_orthogonalise(desc, t, o, ws)
+    assert torch.equal(*out)
