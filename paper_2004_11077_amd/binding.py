@@ -535,8 +535,35 @@ def _room(workspace):
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
+_types = None
+
+
+def _fit(*tensors):
+    """Refuses tensors that a kernel would read or write past their end, or on another device than
+    the current one: (name, tensor or None, TYPE_* or a torch type, least number of elements)."""
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.cuda.current_device, {TYPE_F32: torch.float32, TYPE_BF16: torch.bfloat16,
+                                              TYPE_I8: torch.int8, "i64": torch.int64})
+    device = _types[0]()
+    for name, t, kind, least in tensors:
+        if t is None:
+            continue
+        dtype = _types[1].get(kind)
+        if dtype is not None and t.dtype is not dtype:      # an unknown type is the library's to refuse
+            raise WinoError(-1, "%s is %s, the descriptor says %s" % (name, t.dtype, dtype))
+        if t.numel() < least:
+            raise WinoError(-1, "%s has %d elements, %d needed" % (name, t.numel(), least))
+        if t.get_device() != device:
+            raise WinoError(-1, "%s is not on the current device" % name)
+
+
 def wino_layer_norm(desc, x, gamma, beta, y, mean=None, rstd=None, stream=None):
     """Layer norm of the rows of ``x``; gamma, beta, mean and rstd may be None."""
+    n, c = desc.rows, desc.channels
+    _fit(("x", x, desc.x_type, n * c), ("gamma", gamma, TYPE_F32, c), ("beta", beta, TYPE_F32, c),
+         ("y", y, desc.y_type, n * c), ("mean", mean, TYPE_F32, n), ("rstd", rstd, TYPE_F32, n))
     _check(_load().wino_layer_norm(C.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y),
                                    _ptr(mean), _ptr(rstd), _stream(stream)))
     return y
@@ -549,6 +576,10 @@ def wino_layer_norm_backward_workspace_bytes(desc):
 def wino_layer_norm_backward(desc, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace,
                              stream=None):
     """Gradients of wino_layer_norm; each of dx, dgamma and dbeta may be None."""
+    n, c = desc.rows, desc.channels
+    _fit(("dy", dy, desc.g_type, n * c), ("x", x, desc.x_type, n * c), ("gamma", gamma, TYPE_F32, c),
+         ("mean", mean, TYPE_F32, n), ("rstd", rstd, TYPE_F32, n), ("dx", dx, desc.g_type, n * c),
+         ("dgamma", dgamma, TYPE_F32, c), ("dbeta", dbeta, TYPE_F32, c), ("workspace", workspace, None, 0))
     _check(_load().wino_layer_norm_backward(C.byref(desc), _ptr(dy), _ptr(x), _ptr(gamma),
                                             _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma),
                                             _ptr(dbeta), _ptr(workspace), _room(workspace),
@@ -562,6 +593,10 @@ def wino_linear_cross_entropy_workspace_bytes(desc):
 
 def wino_linear_cross_entropy(desc, h, w, bias, targets, loss, lse, workspace, stream=None):
     """Loss and log-sum-exp of every row; bias may be None, targets are int64."""
+    t, d, v = desc.rows, desc.features, desc.classes
+    _fit(("h", h, desc.type, t * d), ("w", w, desc.type, v * d if t else 0), ("bias", bias, TYPE_F32, v),
+         ("targets", targets, "i64", t), ("loss", loss, TYPE_F32, t), ("lse", lse, TYPE_F32, t),
+         ("workspace", workspace, None, 0))
     _check(_load().wino_linear_cross_entropy(C.byref(desc), _ptr(h), _ptr(w), _ptr(bias),
                                              _ptr(targets), _ptr(loss), _ptr(lse), _ptr(workspace),
                                              _room(workspace), _stream(stream)))
@@ -575,6 +610,11 @@ def wino_linear_cross_entropy_backward_workspace_bytes(desc):
 def wino_linear_cross_entropy_backward(desc, h, w, bias, targets, lse, dloss, dh, dw, dbias,
                                        workspace, stream=None):
     """Gradients of wino_linear_cross_entropy; each of dh, dw and dbias may be None."""
+    t, d, v = desc.rows, desc.features, desc.classes
+    _fit(("h", h, desc.type, t * d), ("w", w, desc.type, v * d if t else 0), ("bias", bias, TYPE_F32, v),
+         ("targets", targets, "i64", t), ("lse", lse, TYPE_F32, t), ("dloss", dloss, TYPE_F32, t),
+         ("dh", dh, desc.type, t * d), ("dw", dw, desc.type, v * d), ("dbias", dbias, TYPE_F32, v),
+         ("workspace", workspace, None, 0))
     _check(_load().wino_linear_cross_entropy_backward(
         C.byref(desc), _ptr(h), _ptr(w), _ptr(bias), _ptr(targets), _ptr(lse), _ptr(dloss),
         _ptr(dh), _ptr(dw), _ptr(dbias), _ptr(workspace), _room(workspace), _stream(stream)))
@@ -587,6 +627,8 @@ def wino_orthogonalise_workspace_bytes(desc):
 
 def wino_orthogonalise(desc, g, o, workspace, stream=None):
     """Orthogonalised updates of a batch of weight gradients."""
+    n = desc.batch * desc.rows * desc.cols
+    _fit(("g", g, desc.g_type, n), ("o", o, desc.o_type, n), ("workspace", workspace, None, 0))
     _check(_load().wino_orthogonalise(C.byref(desc), _ptr(g), _ptr(o), _ptr(workspace),
                                       _room(workspace), _stream(stream)))
     return o

@@ -33,8 +33,8 @@ constexpr float kInf = __builtin_inff();
 // Numbers that kernels hand to later ones.
 struct Numbers {
   float ref;              // largest |dloss|
-  float of_w, of_h;       // what a value in W's, h's planes has to be multiplied by
-  float pad;
+  int of_w, of_h;         // exponents of W's, h's planes: they hold 2^e times the values
+  int pad;
   float max_w[kRange], max_h[kRange];
 };
 
@@ -122,8 +122,8 @@ struct Copy {
   uint16_t* dst;
   int ld;
   int masked;             // rows that do not count as zeros
-  const float* most;      // fp32: [kRange] partial maxima; null: one power of two a row, to `unit`
-  float* unit;
+  const float* most;      // fp32: [kRange] partial maxima; null: one power of two a row
+  int* exponent;          // the one or the rows'
 };
 
 template <class T, int NP>
@@ -132,7 +132,7 @@ __device__ __forceinline__ void copy_rows(const Copy& o, const Rows& g, unsigned
   if constexpr (NP == 2) {
     const int e = exponent_for(group_max(o.most[threadIdx.x], lds));
     scale = power(e);
-    if (block == 0 && threadIdx.x == 0) *o.unit = power(-e);
+    if (block == 0 && threadIdx.x == 0) *o.exponent = e;
   }
   const unsigned each = o.ld / 8;
   const long items = (long)o.rows * each;
@@ -172,7 +172,7 @@ __device__ __forceinline__ void copy_rows_apart(const Copy& o, unsigned block, u
     for (int d = 1; d < 64; d *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, d, 64));
     const int e = exponent_for(m);
     const float scale = power(e);
-    if (lane == 0) o.unit[r] = power(-e);
+    if (lane == 0) o.exponent[r] = e;
     for (int c = lane * 2; c < o.ld; c += 128) {
       uint16_t a[2], b[2];
       cut<2>(c < o.cols ? p[c] * scale : 0.f, a);
@@ -201,8 +201,8 @@ struct Logits {
   Rows g;
   int first, count;          // classes of this piece
   int k;                     // features in whole blocks
-  const float* of_w;         // fp32: the planes' units, one for all rows or (apart) one a row
-  const float* of_h;
+  const int* of_w;           // fp32: the planes' exponents, one for all rows or (apart) one a row
+  const int* of_h;
   int apart;
 };
 
@@ -210,13 +210,13 @@ struct Logits {
 template <class T>
 __device__ __forceinline__ void to_logits(const Logits& g, int v0, int j_t, f32x4 (&acc)[T::TM][T::TN], int j) {
   if constexpr (T::NP == 2) {
-    const float u = g.of_h[g.apart ? j_t : 0];
+    const int u = g.of_h[g.apart ? j_t : 0];
 #pragma unroll
     for (int i = 0; i < T::TM; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int v = v0 + i * 16 + e;
-        acc[i][j][e] *= g.of_w[!g.apart ? 0 : v < g.count ? v : g.count - 1] * u;
+        acc[i][j][e] = __builtin_ldexpf(acc[i][j][e], -(u + g.of_w[!g.apart ? 0 : v < g.count ? v : g.count - 1]));
       }
   }
   if (g.bias || v0 + T::TM * 16 > g.count) {
@@ -435,7 +435,8 @@ struct Product {
   long split;            // elements between ranges of k
   int kind, k, per;      // k in all and per range
   int count, width;      // rows and features of out
-  const float *ref, *unit;
+  const float* ref;
+  const int* exponent;   // of the features' planes
 };
 template <class T, bool FOUR>
 __device__ __forceinline__ void make_product(const Product& p, int group, int groups, int range, char* lds) {
@@ -457,8 +458,7 @@ __device__ __forceinline__ void make_product(const Product& p, int group, int gr
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave % T::WM, wn = wave / T::WM;
   const float scale = p.kind < 2 ? *p.ref : 1.f;
-  float unit = 1.f;
-  if constexpr (T::NP == 2) unit = *p.unit * (1.f / (1 << kDlExponent));
+  const int e2 = T::NP == 2 ? -(*p.exponent + kDlExponent) : 0;
   const long base = range * p.split;
 #pragma unroll
   for (int i = 0; i < T::TM; ++i) {
@@ -470,7 +470,7 @@ __device__ __forceinline__ void make_product(const Product& p, int group, int gr
       if (n >= all_n) continue;
       f32x4 v = acc[i][j];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = v[e] * unit * scale;
+      for (int e = 0; e < 4; ++e) v[e] = (T::NP == 2 ? __builtin_ldexpf(v[e], e2) : v[e]) * scale;
       if constexpr (FOUR) {
         const long at = base + (long)n * p.width + m;
         if (p.kind == 1) {
@@ -593,9 +593,9 @@ void operands(const LossArgs& a, const LossLayout& l, const Rows& g, const void*
   uint16_t* to_h = reinterpret_cast<uint16_t*>(ws + l.h);
   const long pw = (long)count * l.dp / 8, ph = (long)a.rows * l.dp / 8;
   const Copy cw{w_rows, a.w_stride, count, a.features, to_w, l.dp, 0, back ? num->max_w : nullptr,
-                back ? &num->of_w : reinterpret_cast<float*>(ws + l.unit_w)};
+                back ? &num->of_w : reinterpret_cast<int*>(ws + l.unit_w)};
   const Copy ch{h, a.h_stride, a.rows, a.features, to_h, l.dp, back, back ? num->max_h : nullptr,
-                back ? &num->of_h : reinterpret_cast<float*>(ws + l.unit_h)};
+                back ? &num->of_h : reinterpret_cast<int*>(ws + l.unit_h)};
   // a wave a row, or a thread eight values
   const auto grid = [&](long rows, long eights) { return NP == 2 && !back ? grid_of(rows * 64, 2048) : grid_of(eights, 2048); };
   const unsigned first = w_direct ? 0 : grid(count, pw), more = h_ready ? 0 : grid(a.rows, ph);
@@ -621,7 +621,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
   const long most = (1L << 21) / ((a.rows + 63) / 64) * 64;
   long piece = w_direct ? a.classes : l.piece;
   if (piece > most) piece = most < 256 ? 256 : most / 256 * 256;
-  Logits q{bias, g, 0, 0, l.dp, reinterpret_cast<const float*>(ws + l.unit_w), reinterpret_cast<const float*>(ws + l.unit_h), 1};
+  Logits q{bias, g, 0, 0, l.dp, reinterpret_cast<const int*>(ws + l.unit_w), reinterpret_cast<const int*>(ws + l.unit_h), 1};
   int part = 0;
   for (long first = 0; first < a.classes; first += piece) {
     q.first = (int)first;
