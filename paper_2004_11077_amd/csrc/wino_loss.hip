@@ -14,7 +14,8 @@
 // not average out, or small products to two bf16 values: one row of two classes was off by 0.004 of the
 // gradient, twice a bf16 result's rounding).  fp32 operands become two
 // fp16 planes (22 bits) under one power of two for W and one for h (in the forward pass one a row, so that
-// no row's magnitude touches another's lse); in the backward pass rows that are left out count as
+// no row's magnitude touches another's lse; of few rows and large W fp32 as it stands, cut between
+// LDS and the matrix instructions: W is then read and nothing else); in the backward pass rows that are left out count as
 // zeros, whatever they hold, and do not enter the power of two.  dl is kept relative to the largest
 // |dloss|, by which the products' results are multiplied in fp32: with one weight for all rows, as
 // for a mean, the -1 of a target's class stays free of a rounding that would be the same in every row.
@@ -92,11 +93,20 @@ __device__ __forceinline__ float range_of(const float* x, long ld, int rows, int
 }
 
 // First kernel of a backward pass: the largest |dloss| of the rows that count, and for fp32 the ranges of W and
-// of h's rows that count.
+// of h's rows that count, or a copy of h in which the other rows are zeros.
 __global__ __launch_bounds__(1024) void k_loss_range(const float* __restrict__ w, long w_ld,
                                                      const float* __restrict__ h, long h_ld, int features, Rows g,
-                                                     const float* __restrict__ dloss, Numbers* __restrict__ to) {
+                                                     const float* __restrict__ dloss, Numbers* __restrict__ to,
+                                                     float* __restrict__ copy) {
   __shared__ float lds[16];
+  if (copy) {
+    for (int r = blockIdx.x; r < g.rows; r += gridDim.x) {
+      const bool kept = g.kept(r);
+      for (int c = threadIdx.x; c < features; c += 1024)
+        copy[(long)r * features + c] = kept ? h[(long)r * h_ld + c] : 0.f;
+    }
+    h = nullptr;
+  }
   if (dloss && blockIdx.x == 0) {
     float m = 0;
     for (int t = threadIdx.x; t < g.rows; t += 1024)
@@ -378,17 +388,24 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
       if (near)
 #pragma unroll
         for (int e = 0; e < 4; ++e) d[e] -= off == i * 16 + e ? 1.f : 0.f;
-      uint16_t out[4][T::NP];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        // a row that is left out gives zeros, whatever its logits are
-        d[e] = weight == 0.f ? 0.f : d[e] * weight;
-        if constexpr (T::NP == 2) cut<2>(d[e] * (float)(1 << kDlExponent), out[e]);
-        else cut<1>(d[e], out[e]);
-      }
+      for (int e = 0; e < 4; ++e) d[e] = weight == 0.f ? 0.f : d[e] * weight;   // of a row that is left out: zeros
       acc[i][j] = d;
       const int v = v0 + i * 16;
-      if (t < g.g.rows && v < ld) {   // ld is a multiple of 4; from the last class on d is zero
+      if (t >= g.g.rows || v >= ld) continue;   // ld is a multiple of 4; from the last class on d is zero
+      // tiles of 32 end where the line's last ones have no rows of W: zeros behind them
+      const bool pad = is_few<T> && tm + 1 == tiles_m && v + 32 < ld;
+      if constexpr (T::NP == 3) {
+        float* to = reinterpret_cast<float*>(dl) + (long)t * ld + v;
+        *reinterpret_cast<f32x4*>(to) = d;
+        if (pad) *reinterpret_cast<f32x4*>(to + 32) = f32x4{0, 0, 0, 0};
+      } else {
+        uint16_t out[4][T::NP];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (T::NP == 2) cut<2>(d[e] * (float)(1 << kDlExponent), out[e]);
+          else cut<1>(d[e], out[e]);
+        }
 #pragma unroll
         for (int p = 0; p < T::NP; ++p)
           *reinterpret_cast<ushort4*>(dl + (long)t * ld * T::NP + place<T::NP>(v) + p * 32) =
@@ -397,13 +414,12 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
           *reinterpret_cast<ushort4*>(rest + (long)t * ld + v) =
               make_ushort4(bf16_bits(d[0] - bf16_value(out[0][0])), bf16_bits(d[1] - bf16_value(out[1][0])),
                            bf16_bits(d[2] - bf16_value(out[2][0])), bf16_bits(d[3] - bf16_value(out[3][0])));
-        // tiles of 32 end where the line's last ones have no rows of W: zeros behind them
-        if (is_few<T> && tm + 1 == tiles_m && v + 32 < ld)
+        if (pad) {
 #pragma unroll
           for (int p = 0; p < T::NP; ++p)
             *reinterpret_cast<ushort4*>(dl + (long)t * ld * T::NP + place<T::NP>(v + 32) + p * 32) = make_ushort4(0, 0, 0, 0);
-        if (is_few<T> && T::NP == 1 && rest && tm + 1 == tiles_m && v + 32 < ld)
-          *reinterpret_cast<ushort4*>(rest + (long)t * ld + v + 32) = make_ushort4(0, 0, 0, 0);
+          if (T::NP == 1 && rest) *reinterpret_cast<ushort4*>(rest + (long)t * ld + v + 32) = make_ushort4(0, 0, 0, 0);
+        }
       }
     }
   }
@@ -558,26 +574,38 @@ struct Tiles {
 };
 constexpr long kDeepGroups = 512;
 long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
-// The same of products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the
-// waves where there are few tiles.
+// Products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the waves where
+// there are few tiles.
+int least_side(long m, long n, long k) { return count_of(m, n, 64) < 64 && k >= 256 ? 32 : 64; }
 int side_along(long m, long n, long k) {
   const int side = side_for(m, n, 1);
-  return side == 64 && count_of(m, n, 64) < 64 && k >= 256 ? 32 : side;
+  return side == 64 ? least_side(m, n, k) : side;
 }
 constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
 
 template <int NP, bool AX, bool BX, class F>
 void with_tile(int side, long groups, F&& f) {
-  if (side == 256) f(typename Tiles<NP, AX, BX>::Big{});
-  else if (side == 32 && !AX && !BX) f(Few<NP>{});
-  else if (side == 128) f(typename Tiles<NP, AX, BX>::Mid{});
-  else if (groups <= kDeepGroups) f(typename Tiles<NP, AX, BX>::Deep{});
+  if constexpr (NP < 3) {
+    if (side == 256) return f(typename Tiles<NP, AX, BX>::Big{});
+    if (side == 128) return f(typename Tiles<NP, AX, BX>::Mid{});
+  }
+  if constexpr (!AX && !BX)
+    if (side == 32) return f(Few<NP>{});
+  if (groups <= kDeepGroups) f(typename Tiles<NP, AX, BX>::Deep{});
   else f(typename Tiles<NP, AX, BX>::Small{});
 }
 
 // bf16 rows that the products can take where they lie: 16-byte accesses, whole stages of k.
 bool direct(const LossArgs& a, const void* p, long stride) {
   return a.bf16 && a.features % 64 == 0 && stride % 8 == 0 && stride <= kMaxLd && ((uintptr_t)p & 15) == 0;
+}
+
+// fp32 as it stands: few rows, where the time is W's passage through memory (75113 x 925 and 3 rows, a
+// training step: 951 us by way of planes).  Values below 2^-102 lose lower pieces to bf16's smallest
+// numbers there, so smaller weights keep to the planes.
+bool as_it_stands(const LossArgs& a) {
+  return !a.bf16 && a.rows <= 64 && (double)a.features * a.classes >= 1 << 22 && a.h_stride <= kMaxLd / 2 &&
+         a.w_stride <= kMaxLd / 2;
 }
 
 const void* row_at(const LossArgs& a, const void* p, long row, long stride) {
@@ -589,6 +617,11 @@ template <int NP>
 void operands(const LossArgs& a, const LossLayout& l, const Rows& g, const void* w_rows, int count, const void* h,
               bool w_direct, bool h_ready, bool back, Numbers* num, char* ws, Operand* ow, Operand* oh,
               hipStream_t st) {
+  if constexpr (NP == 3) {
+    *ow = Operand{(const uint16_t*)w_rows, a.w_stride * 2, 0, count, a.features};
+    *oh = back ? Operand{(const uint16_t*)(ws + l.h), a.features * 2L, 0, a.rows, a.features}
+               : Operand{(const uint16_t*)h, a.h_stride * 2, 0, a.rows, a.features};
+  } else {
   uint16_t* to_w = reinterpret_cast<uint16_t*>(ws + l.w);
   uint16_t* to_h = reinterpret_cast<uint16_t*>(ws + l.h);
   const long pw = (long)count * l.dp / 8, ph = (long)a.rows * l.dp / 8;
@@ -604,6 +637,7 @@ void operands(const LossArgs& a, const LossLayout& l, const Rows& g, const void*
   *ow = w_direct ? Operand{(const uint16_t*)w_rows, a.w_stride, 0, count, a.features}
                  : Operand{to_w, (long)l.dp * NP, 0, count, l.dp};
   if (!h_ready) *oh = Operand{to_h, (long)l.dp * NP, 0, a.rows, l.dp};
+  }
 }
 
 template <int NP>
@@ -619,7 +653,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
   Operand oh{(const uint16_t*)h, a.h_stride, 0, a.rows, a.features}, ow{};
   // a launch holds fewer than 2^32 threads
   const long most = (1L << 21) / ((a.rows + 63) / 64) * 64;
-  long piece = w_direct ? a.classes : l.piece;
+  long piece = w_direct || NP == 3 ? a.classes : l.piece;
   if (piece > most) piece = most < 256 ? 256 : most / 256 * 256;
   Logits q{bias, g, 0, 0, l.dp, reinterpret_cast<const int*>(ws + l.unit_w), reinterpret_cast<const int*>(ws + l.unit_h), 1};
   int part = 0;
@@ -628,7 +662,8 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
     q.count = (int)(a.classes - first < piece ? a.classes - first : piece);
     operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, num, ws, &ow, &oh, st);
     h_ready = true;
-    with_tile<NP, false, false>(side_along(q.count, a.rows, l.dp), count_of(q.count, a.rows, 64), [&](auto tile) {
+    with_tile<NP, false, false>(NP == 3 ? least_side(q.count, a.rows, l.dp) : side_along(q.count, a.rows, l.dp),
+                                count_of(q.count, a.rows, 64), [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
       const bool all = tm == 1 && q.count == a.classes;
@@ -656,8 +691,9 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
   Numbers* num = reinterpret_cast<Numbers*>(ws + l.numbers);
   const float* ref = &num->ref;
   const Rows g{target, a.ignore_index, a.rows, a.classes};
-  wino_launch(k_loss_range, dim3(NP == 2 ? kRange : 1), dim3(1024), st, NP == 2 ? (const float*)w : nullptr, a.w_stride,
-              NP == 2 ? (const float*)h : nullptr, a.h_stride, a.features, g, dloss, num);
+  wino_launch(k_loss_range, dim3(NP == 1 ? 1 : kRange), dim3(1024), st, NP == 2 ? (const float*)w : nullptr, a.w_stride,
+              NP == 1 ? nullptr : (const float*)h, a.h_stride, a.features, g, dloss, num,
+              NP == 3 ? reinterpret_cast<float*>(ws + l.h) : nullptr);
   const bool w_direct = direct(a, w, a.w_stride);
   bool h_ready = false;   // always a copy: rows that are left out as zeros
   Operand oh{}, ow{};
@@ -681,7 +717,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
       wino_launch((k_loss_dlogits<T>), dim3(tm * tn), dim3(T::THREADS), st, ow, oh, q, tm, tn, lse, dloss, ref, dl, vp,
                   rest, db);
     });
-    const Operand od{dl, (long)vp * NP, 0, a.rows, vp};
+    const Operand od{dl, (long)vp * (NP == 1 ? 1 : 2), 0, a.rows, vp};
     const int per = (int)up((vp + l.splits - 1) / l.splits, 64), tk = (int)up(a.rows, 64);
     const int dw_per = (int)up((tk + l.dw_splits - 1) / l.dw_splits, 64);
     float* dw_sums = l.dw_splits > 1 ? reinterpret_cast<float*>(ws + l.dw) : nullptr;
@@ -691,7 +727,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
                      a.rows, a.features, ref, &num->of_w};
     const Product pw{od, oh, rest, dw_sums ? (void*)dw_sums : dw_rows, dw_items, dw_sums ? 2 : a.bf16, tk, dw_per, q.count,
                      a.features, ref, &num->of_h};
-    const int dw_side = dw_sums ? 64 : side_for(q.count, a.features, 1);
+    const int dw_side = dw_sums || NP == 3 ? 64 : side_for(q.count, a.features, 1);
     const auto tiles = [](const Product& p, int side) { return (int)count_of(p.count, p.width, side); };
     if (dh && dw && l.dh_side == 64 && dw_side == 64) {
       const int th = tiles(ph, 64), tw = tiles(pw, 64), all = th * l.splits;
@@ -773,12 +809,13 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
     // two bf16 values
     l.two = a.bf16 && (T <= 64 || (double)T * D * V <= 1 << 30);
     if (l.two) l.rest = take(item * T * vp);
-    l.side = side_along((long)P, (long)T, l.dp);
+    const bool stands = as_it_stands(a);
+    l.side = stands ? least_side((long)P, (long)T, l.dp) : side_along((long)P, (long)T, l.dp);
     // ranges of classes, each of 512 or more, until dh's tiles fill the chip: one tile of 256 a compute
     // unit, or two of the smaller ones
     const long room = (long)(vp / 512 ? vp / 512 : 1);
     double most = 0;
-    for (int side = 256; side >= 64 && T; side /= 2) {
+    for (int side = stands ? 64 : 256; side >= 64 && T; side /= 2) {
       const long tiles = count_of((long)D, (long)T, side), slots = side == 256 ? 256 : 512;
       long ranges = slots / tiles;
       ranges = ranges > room ? room : ranges < 1 ? 1 : ranges;
@@ -802,7 +839,8 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
 hipError_t launch_loss(const LossArgs& a, const void* h, const void* w, const float* bias,
                        const int64_t* target, float* loss, float* lse, char* ws, hipStream_t st) {
   return a.bf16 ? forward<1>(a, h, w, bias, target, loss, lse, ws, st)
-                : forward<2>(a, h, w, bias, target, loss, lse, ws, st);
+       : as_it_stands(a) ? forward<3>(a, h, w, bias, target, loss, lse, ws, st)
+                         : forward<2>(a, h, w, bias, target, loss, lse, ws, st);
 }
 
 hipError_t launch_loss_backward(const LossArgs& a, const void* h, const void* w, const float* bias,
@@ -816,7 +854,8 @@ hipError_t launch_loss_backward(const LossArgs& a, const void* h, const void* w,
     return hipGetLastError();
   }
   return a.bf16 ? backward<1>(a, h, w, bias, target, lse, dloss, dh, dw, dbias, ws, st)
-                : backward<2>(a, h, w, bias, target, lse, dloss, dh, dw, dbias, ws, st);
+       : as_it_stands(a) ? backward<3>(a, h, w, bias, target, lse, dloss, dh, dw, dbias, ws, st)
+                         : backward<2>(a, h, w, bias, target, lse, dloss, dh, dw, dbias, ws, st);
 }
 
 }  // namespace wino

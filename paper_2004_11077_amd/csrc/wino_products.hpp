@@ -9,7 +9,10 @@
 // holds); what is smaller than 2^-18 of that keeps 2^-40 of it.  Products of two such values are exact
 // in fp32, so a sum is as good as one of fp32 products (measured against 64 bits: better, because a
 // block of 32 k costs three roundings of the sum and not 32), at three matrix instructions of 2.5
-// PFLOP/s instead of one fp32 instruction of 0.157 PFLOP/s.
+// PFLOP/s instead of one fp32 instruction of 0.157 PFLOP/s.  NP = 3: fp32 values as they stand, cut into
+// three bf16 values of 8 bits each when they are read from LDS, and six of nine products: twice the
+// instructions and the cutting for every tile, but no planes to be written and read and no power of two
+// to be known.  It is for operands that are read about once.
 //
 // Two planes lie together, 32 elements of the one and then 32 of the other: 128 bytes, a cache line.
 //
@@ -49,7 +52,7 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 constexpr long kMaxLd = 1L << 21;   // elements between rows: 256 rows of it are 2^30 bytes
 
 // One operand: `rows` rows of `cols` elements, batch b, row r at p + b batch + r ld, element e of plane q
-// there at place<NP>(e) + 32 q.  k along the rows: m or n is r, k is e.  Across: k is r, m or n is e.
+// there at place<NP>(e) + 32 q; fp32 (NP = 3): at 2 e, strides in 16-bit units too.  k along the rows: m or n is r, k is e.  Across: k is r, m or n is e.
 struct Operand {
   const uint16_t* p;
   long ld, batch;
@@ -74,6 +77,21 @@ __device__ __forceinline__ void cut(float x, uint16_t (&out)[NP]) {
   } else {
     out[0] = f16_bits(x);
     out[1] = f16_bits(x - f16_value(out[0]));
+  }
+}
+
+// Eight fp32 values as three times eight bf16 values: the upper 8 bits cut off, so that nothing overflows,
+// the rest rounded, and what is then left, which is a bf16 value: together x exactly.
+__device__ __forceinline__ void cut_three(const f32x4 (&x)[2], u32x4 (&out)[3]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = x[i >> 1][(i & 1) * 2], b = x[i >> 1][(i & 1) * 2 + 1];
+    const uint32_t ha = __builtin_bit_cast(uint32_t, a) & 0xffff0000u, hb = __builtin_bit_cast(uint32_t, b) & 0xffff0000u;
+    const float ra = a - __builtin_bit_cast(float, ha), rb = b - __builtin_bit_cast(float, hb);
+    const uint16_t ma = bf16_bits(ra), mb = bf16_bits(rb);
+    out[0][i] = ha >> 16 | hb;
+    out[1][i] = ma | (uint32_t)mb << 16;
+    out[2][i] = bf16_bits(ra - bf16_value(ma)) | (uint32_t)bf16_bits(rb - bf16_value(mb)) << 16;
   }
 }
 
@@ -125,7 +143,7 @@ struct Tile {
   static constexpr bool AX = AX_, BX = BX_;                    // k across the rows of A, of B
   static constexpr int NW = WM * WN, THREADS = 64 * NW;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;   // 16 x 16 blocks per wave
-  static constexpr int K = 64 / NP;                            // k of a stage
+  static constexpr int K = NP == 1 ? 64 : 32;                  // k of a stage
   static constexpr int RA = BM / 8, RB = BN / 8;               // KiB of a stage of the operands
   static constexpr int STAGE = (RA + RB) * 1024;               // bytes
   static constexpr int LDS = RING * STAGE;
@@ -142,7 +160,7 @@ struct Tile {
 template <int NP_, int WAVES_ = 4>
 struct Few {
   static constexpr int BM = 32, BN = 32, WM = 2, WN = 2, NP = NP_, WAVES = WAVES_, TM = 1, TN = 1;
-  static constexpr int THREADS = 64 * WAVES, K = 64 / NP, LDS = WAVES * 4096;
+  static constexpr int THREADS = 64 * WAVES, K = NP == 1 ? 64 : 32, LDS = WAVES * 4096;
 };
 template <class T>
 constexpr bool is_few = false;
@@ -170,23 +188,26 @@ __device__ __forceinline__ int swap_of(int k) { return ((k >> 1) & 1) * 2 + ((k 
 // One operand's side of a tile: SIDE rows (m or n), X: k across.
 template <int SIDE, bool X, int NP, int NW>
 struct Side {
-  static constexpr int K = 64 / NP, KG = K / 8, N = SIDE / 8 / NW;
+  static constexpr int K = NP == 1 ? 64 : 32, KG = K / 8, N = SIDE / 8 / NW;
+  static constexpr int UNITS = NP == 1 ? 1 : 2;   // 16-bit units of an element
+  static constexpr int PARTS = NP == 3 ? 3 : 2;   // what a fragment comes in
   const uint16_t* base;
   long bytes, step;          // from the base to the operand's end; across: elements of a stage
   __amdgpu_buffer_rsrc_t rsrc;
   int at[N];                 // a copy's source, in bytes from the base
   int read[X ? 4 : 2];       // a lane's places in a stage
+  int cols;
 
   __device__ __forceinline__ Side(const Operand& o, long batch, int first, int k, int lane, int wave) {
-    const long start = X ? (long)k * o.ld + first * NP : (long)first * o.ld;
+    const long start = X ? (long)k * o.ld + first * UNITS : (long)first * o.ld;
     base = o.p + batch * o.batch + start;
     if constexpr (X) {
-      bytes = ((long)(o.rows - 1) * o.ld + (long)o.cols * NP - start) * 2;
+      bytes = ((long)(o.rows - 1) * o.ld + (long)o.cols * UNITS - start) * 2;
       step = K * o.ld;
     } else {
       int rows = o.rows - first;
       rows = rows < SIDE ? rows : SIDE;
-      bytes = ((long)(rows - 1) * o.ld + (long)o.cols * NP) * 2;
+      bytes = ((long)(rows - 1) * o.ld + (long)o.cols * UNITS) * 2;
       step = 0;
       rsrc = window(base, bytes);
     }
@@ -202,14 +223,22 @@ struct Side {
         at[i] = ((block * 8 + (lane >> 3)) * (int)o.ld + ((lane & 7) ^ (lane >> 3)) * 8) * 2;
       }
     }
-    if constexpr (X) {
+    cols = o.cols;
+    if constexpr (X && NP == 3) {
+      // place i: half i / 2 of 32 values, rows with bit 1 of k as i % 2
+      const int g = lane >> 4, e = lane & 15;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        read[i] = g * 1024 + (((i >> 1) * 4 + (e >> 2)) ^ ((i & 1) * 2 + (g & 1) * 4)) * 16 + (e & 3) * 4;
+    } else if constexpr (X) {
       const int g = lane >> 4, r = (lane >> 2) & 3, q = lane & 3, swap = swap_of(g * 8 + r);
 #pragma unroll
       for (int i = 0; i < 4; ++i) read[i] = g * 1024 + r * 128 + ((i * 2 + (q >> 1)) ^ swap) * 16 + (q & 1) * 8;
     } else {
       const int r = lane & 7;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) read[i] = (lane & 15) * 128 + ((i * 4 + (lane >> 4)) ^ r) * 16;
+      for (int i = 0; i < 2; ++i)
+        read[i] = (lane & 15) * 128 + ((NP == 3 ? (lane >> 4) * 2 + i : i * 4 + (lane >> 4)) ^ r) * 16;
     }
   }
 
@@ -219,39 +248,62 @@ struct Side {
 #pragma unroll
     for (int i = 0; i < N; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc, (__attribute__((address_space(3))) void*)(to + (i * NW + wave) * 1024), 16, at[i], X ? 0 : k * 2 * NP, 0, 0);
+          rsrc, (__attribute__((address_space(3))) void*)(to + (i * NW + wave) * 1024), 16, at[i], X ? 0 : k * 2 * UNITS, 0, 0);
     if constexpr (X) {
       base += step;
       bytes -= step * 2;
     }
   }
 
-  // What the instruction takes of 16 rows `block` of part `sub` of a stage: its 32 k of one plane or its plane.
-  __device__ __forceinline__ u32x4 fragment(const char* from, int sub, int block) const {
-    if constexpr (X) {
-      typedef __attribute__((address_space(3))) s16x4 L;
-      const char* p = NP == 1 ? from + ((block >> 2) * 8 + sub * 4) * 1024 + read[block & 3]
-                              : from + (block >> 1) * 4096 + read[sub * 2 + (block & 1)];
-      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p));
-      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(p + 512)));
-      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  // What the instruction takes of 16 rows `block` of the stage at k: the two parts of 32 k of one plane, the two
+  // planes, or the three pieces of fp32 values.
+  __device__ __forceinline__ void fragment(const char* from, int block, int k, int lane, u32x4 (&out)[PARTS]) const {
+    if constexpr (NP == 3) {
+      f32x4 x[2];
+      if constexpr (X) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          x[j >> 2][j & 3] = *reinterpret_cast<const float*>(from + (block >> 1) * 4096 + j * 128 + read[(block & 1) * 2 + ((j >> 1) & 1)]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const f32x4*>(from + block * 2048 + read[i]);
+        if (k + 32 > cols)   // the next row's values, or nothing's
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (k + (lane >> 4) * 8 + e >= cols) x[e >> 2][e & 3] = 0;
+      }
+      cut_three(x, out);
     } else {
-      return *reinterpret_cast<const u32x4*>(from + block * 2048 + read[sub]);
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        if constexpr (X) {
+          typedef __attribute__((address_space(3))) s16x4 L;
+          const char* p = NP == 1 ? from + ((block >> 2) * 8 + sub * 4) * 1024 + read[block & 3]
+                                  : from + (block >> 1) * 4096 + read[sub * 2 + (block & 1)];
+          const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p));
+          const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(p + 512)));
+          out[sub] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+          out[sub] = *reinterpret_cast<const u32x4*>(from + block * 2048 + read[sub]);
+        }
+      }
     }
   }
 };
 #endif
 
-// Two planes: upper and lower, lower and upper, upper and upper; one: its two parts of 32 k each.
-template <int NP, int TM, int TN>
-__device__ __forceinline__ void multiply_parts(const u32x4 (&a)[2][TM], const u32x4 (&b)[2][TN], f32x4 (&acc)[TM][TN]) {
+// Two planes: upper and lower, lower and upper, upper and upper; one: its two parts of 32 k each; three
+// pieces: the six largest products, the smallest first.
+template <int NP, int TM, int TN, int PARTS>
+__device__ __forceinline__ void multiply_parts(const u32x4 (&a)[TM][PARTS], const u32x4 (&b)[TN][PARTS], f32x4 (&acc)[TM][TN]) {
 #pragma unroll
-  for (int s = 0; s < (NP == 1 ? 2 : 3); ++s) {
-    const int p = NP == 1 ? s : s == 1, q = NP == 1 ? s : s == 0;
+  for (int s = 0; s < NP * (NP + 1) / 2 + (NP == 1); ++s) {
+    constexpr int P3[] = {0, 1, 2, 0, 1, 0}, Q3[] = {2, 1, 0, 1, 0, 0};
+    const int p = NP == 1 ? s : NP == 2 ? s == 1 : P3[s], q = NP == 1 ? s : NP == 2 ? s == 0 : Q3[s];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = multiply_block<NP>(a[p][i], b[q][j], acc[i][j]);
+      for (int j = 0; j < TN; ++j) acc[i][j] = multiply_block<NP>(a[i][p], b[j][q], acc[i][j]);
   }
 }
 
@@ -259,18 +311,20 @@ __device__ __forceinline__ void multiply_parts(const u32x4 (&a)[2][TM], const u3
 template <class T>
 __device__ __forceinline__ void multiply_few(const Operand& a, const Operand& b, long batch, int m0, int n0,
                                              int k_begin, int k_end, char* lds, f32x4& out) {
-  constexpr int DEPTH = 4;
+  constexpr int DEPTH = 4, UNITS = T::NP == 1 ? 1 : 2, PARTS = T::NP == 3 ? 3 : 2;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int left_a = a.rows - m0 < 32 ? a.rows - m0 : 32, left_b = b.rows - n0 < 32 ? b.rows - n0 : 32;
-  const auto ra = window(a.p + batch * a.batch + (long)m0 * a.ld, ((left_a - 1) * a.ld + (long)a.cols * T::NP) * 2);
-  const auto rb = window(b.p + batch * b.batch + (long)n0 * b.ld, ((left_b - 1) * b.ld + (long)b.cols * T::NP) * 2);
-  const int at_a = ((lane & 15) * (int)a.ld + (lane >> 4) * 8) * 2, at_b = ((lane & 15) * (int)b.ld + (lane >> 4) * 8) * 2;
+  const auto ra = window(a.p + batch * a.batch + (long)m0 * a.ld, ((left_a - 1) * a.ld + (long)a.cols * UNITS) * 2);
+  const auto rb = window(b.p + batch * b.batch + (long)n0 * b.ld, ((left_b - 1) * b.ld + (long)b.cols * UNITS) * 2);
+  // a lane's two 16-byte pieces of a line: fp32's eight values, or eight of each part
+  constexpr int STEP = T::NP == 3 ? 16 : 8, HALF = T::NP == 3 ? 16 : 64;
+  const int at_a = ((lane & 15) * (int)a.ld + (lane >> 4) * STEP) * 2, at_b = ((lane & 15) * (int)b.ld + (lane >> 4) * STEP) * 2;
   const int next_a = 32 * (int)a.ld, next_b = 32 * (int)b.ld;   // 16 rows on, bytes
   f32x4 acc[2][2] = {};
   const int lines = k_end / T::K;
   for (int l = k_begin / T::K + wave; l < lines; l += DEPTH * T::WAVES) {
-    u32x4 fa[DEPTH][2][2], fb[DEPTH][2][2];
+    u32x4 fa[DEPTH][2][2], fb[DEPTH][2][2];   // [line][16 rows][piece]
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
       // lines beyond the last one: out of the window, zeros
@@ -280,13 +334,31 @@ __device__ __forceinline__ void multiply_few(const Operand& a, const Operand& b,
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int to = off ? 0 : line * 128;
-          fa[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, (at_a + i * next_a + q * 64) | off, to, 0));
-          fb[d][q][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rb, (at_b + i * next_b + q * 64) | off, to, 0));
+          fa[d][i][q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, (at_a + i * next_a + q * HALF) | off, to, 0));
+          fb[d][i][q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rb, (at_b + i * next_b + q * HALF) | off, to, 0));
         }
     }
     __builtin_amdgcn_sched_barrier(0);   // all loads before the first product
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) multiply_parts<T::NP>(fa[d], fb[d], acc);
+    for (int d = 0; d < DEPTH; ++d) {
+      if constexpr (T::NP == 3) {
+        u32x4 pa[2][PARTS], pb[2][PARTS];
+        const auto pieces = [&](const u32x4 (&from)[2], int cols, u32x4 (&out)[PARTS]) {
+          f32x4 x[2] = {__builtin_bit_cast(f32x4, from[0]), __builtin_bit_cast(f32x4, from[1])};
+          const int k = (l + d * T::WAVES) * 32;
+          if (k + 32 > cols)   // the next row's values, or nothing's
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (k + (lane >> 4) * 8 + e >= cols) x[e >> 2][e & 3] = 0;
+          cut_three(x, out);
+        };
+#pragma unroll
+        for (int i = 0; i < 2; ++i) pieces(fa[d][i], a.cols, pa[i]), pieces(fb[d][i], b.cols, pb[i]);
+        multiply_parts<3>(pa, pb, acc);
+      } else {
+        multiply_parts<T::NP>(fa[d], fb[d], acc);
+      }
+    }
   }
   f32x4* join = reinterpret_cast<f32x4*>(lds);   // [wave][block][lane]
 #pragma unroll
@@ -322,15 +394,12 @@ __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, lon
     sa.fetch(k, to, wave);
     sb.fetch(k, to + B_AT, wave);
   };
-  const auto work = [&](const char* from) {
-    u32x4 fa[2][T::TM], fb[2][T::TN];
+  const auto work = [&](const char* from, int k) {
+    u32x4 fa[T::TM][decltype(sa)::PARTS], fb[T::TN][decltype(sb)::PARTS];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int i = 0; i < T::TM; ++i) sa.fragment(from, wm * T::TM + i, k, lane, fa[i]);
 #pragma unroll
-      for (int i = 0; i < T::TM; ++i) fa[q][i] = sa.fragment(from, q, wm * T::TM + i);
-#pragma unroll
-      for (int j = 0; j < T::TN; ++j) fb[q][j] = sb.fragment(from + B_AT, q, wn * T::TN + j);
-    }
+    for (int j = 0; j < T::TN; ++j) sb.fragment(from + B_AT, wn * T::TN + j, k, lane, fb[j]);
     __builtin_amdgcn_s_setprio(1);
     multiply_parts<T::NP>(fa, fb, acc);
     __builtin_amdgcn_s_setprio(0);
@@ -349,7 +418,7 @@ __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, lon
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (t + T::RING - 1 < stages) fetch(k_begin + (t + T::RING - 1) * T::K, lds + next * T::STAGE);
-    work(lds + slot * T::STAGE);
+    work(lds + slot * T::STAGE, k_begin + t * T::K);
     slot = slot + 1 == T::RING ? 0 : slot + 1;
     next = next + 1 == T::RING ? 0 : next + 1;
   }

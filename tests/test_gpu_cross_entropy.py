@@ -130,6 +130,28 @@ def test_strides_and_alignment(D, extra, offset, type):
     check(run(50, D, 300, type, extra=extra, offset=offset), type)
 
 
+@pytest.mark.parametrize("D,extra,offset,V,piece", [(64, 0, 0, 66000, 0), (925, 0, 0, 4700, 0), (515, 5, 3, 8200, 0), (1030, 0, 1, 4100, 1024), (33, 0, 0, 131072, 0)])
+@pytest.mark.parametrize("T", [1, 5, 64])
+def test_few_rows_and_large_weights(T, D, extra, offset, V, piece):
+    """fp32 operands are taken as they stand here, whatever their strides and however many features are left
+    over behind whole blocks of 32."""
+    check(run(T, D, V, "f32", extra=extra, offset=offset, piece=piece, ignored=0.1), "f32")
+
+
+def test_few_rows_beside_rows_left_out():
+    """Large weights, and NaN and infinities in a padding row."""
+    def change(h, w, b, target, dloss):
+        target[[1, 5]] = -100
+        h[1], h[5] = float("nan"), float("inf")
+        dloss[1] = np.nan
+    r = run(9, 130, 33000, "f32", ignored=0, change=change)
+    assert np.isfinite(r["dw"]).all() and np.isfinite(r["dbias"]).all()
+    r["h"][[1, 5]] = 0
+    r["lse"][[1, 5]] = tr.cross_entropy(r["h"], r["w"], r["b"].astype(np.float64), r["target"])[1][[1, 5]]
+    r["dloss"][1] = 0
+    check(r, "f32")
+
+
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 def test_split_classes(type):
     """Few tiles of dh and many classes: ranges of classes are summed apart."""
