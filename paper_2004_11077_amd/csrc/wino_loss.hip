@@ -174,6 +174,7 @@ __device__ __forceinline__ void copy_rows_apart(const Copy& o, unsigned block, u
   for (long r = (long)block * 4 + (threadIdx.x >> 6); r < o.rows; r += (long)blocks * 4) {
     const float* p = static_cast<const float*>(o.src) + r * o.src_ld;
     float m = 0;
+#pragma unroll 8
     for (int c = lane; c < o.cols; c += 64) {
       const float v = __builtin_fabsf(p[c]);
       m = v < kInf ? __builtin_fmaxf(m, v) : m;
@@ -183,6 +184,7 @@ __device__ __forceinline__ void copy_rows_apart(const Copy& o, unsigned block, u
     const int e = exponent_for(m);
     const float scale = power(e);
     if (lane == 0) o.exponent[r] = e;
+#pragma unroll 4
     for (int c = lane * 2; c < o.ld; c += 128) {
       uint16_t a[2], b[2];
       cut<2>(c < o.cols ? p[c] * scale : 0.f, a);
@@ -782,10 +784,10 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
   const int np = a.bf16 ? 1 : 2;
   const size_t item = 2 * (size_t)np;   // bytes of a value in planes
   l.dp = (int)up(D, 64);
-  // classes per piece: what the caller asks for, or as many as keep a piece's dl, and its planes of W,
-  // within 256 MiB
-  const size_t most = T > (size_t)l.dp ? T : (size_t)l.dp;
-  size_t piece = a.piece ? (size_t)a.piece : ((size_t)256 << 20) / (item * most);
+  // classes per piece: what the caller asks for, or as many as keep a piece's dl, and its planes of W if
+  // it may need them, within 256 MiB
+  const size_t most = T > (size_t)l.dp || as_it_stands(a) ? T : (size_t)l.dp;
+  size_t piece = a.piece ? (size_t)a.piece : ((size_t)256 << 20) / (item * (most ? most : 1));
   piece = up(piece < 1024 && !a.piece ? 1024 : piece, 256);
   if (piece > (size_t)kMaxLd / 2) piece = (size_t)kMaxLd / 2;   // rows of dl on two planes
   l.piece = (int)(piece < V ? piece : V);
@@ -793,7 +795,7 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
   size_t at = 0;
   const auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
   l.numbers = take(sizeof(Numbers));
-  l.w = take(item * P * l.dp);
+  if (!as_it_stands(a)) l.w = take(item * P * l.dp);
   l.h = take(item * T * l.dp);
   l.splits = 1;
   if (!back) {
