@@ -48,6 +48,8 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr long kMaxLd = 1L << 21;   // elements between rows: 256 rows of it are 2^30 bytes
 
@@ -80,18 +82,23 @@ __device__ __forceinline__ void cut(float x, uint16_t (&out)[NP]) {
   }
 }
 
+// Two fp32 values as bf16 values, the first in the lower half.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
 // Eight fp32 values as three times eight bf16 values: the upper 8 bits cut off, so that nothing overflows,
-// the rest rounded, and what is then left, which is a bf16 value: together x exactly.
+// the rest rounded, and what is then left, which is a bf16 value: together x exactly.  By pairs: 5.5
+// instructions a value, which are as many of the kernel's cycles as the matrix instructions are.
 __device__ __forceinline__ void cut_three(const f32x4 (&x)[2], u32x4 (&out)[3]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float a = x[i >> 1][(i & 1) * 2], b = x[i >> 1][(i & 1) * 2 + 1];
     const uint32_t ha = __builtin_bit_cast(uint32_t, a) & 0xffff0000u, hb = __builtin_bit_cast(uint32_t, b) & 0xffff0000u;
     const float ra = a - __builtin_bit_cast(float, ha), rb = b - __builtin_bit_cast(float, hb);
-    const uint16_t ma = bf16_bits(ra), mb = bf16_bits(rb);
+    const uint32_t mid = bf16_pair(ra, rb);
     out[0][i] = ha >> 16 | hb;
-    out[1][i] = ma | (uint32_t)mb << 16;
-    out[2][i] = bf16_bits(ra - bf16_value(ma)) | (uint32_t)bf16_bits(rb - bf16_value(mb)) << 16;
+    out[1][i] = mid;
+    out[2][i] = bf16_pair(ra - __builtin_bit_cast(float, mid << 16), rb - __builtin_bit_cast(float, mid & 0xffff0000u));
   }
 }
 
@@ -394,15 +401,26 @@ __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, lon
     sa.fetch(k, to, wave);
     sb.fetch(k, to + B_AT, wave);
   };
-  const auto work = [&](const char* from, int k) {
-    u32x4 fa[T::TM][decltype(sa)::PARTS], fb[T::TN][decltype(sb)::PARTS];
+  const auto some = [&](const char* from, int k, auto& fa, auto& part) {
+    u32x4 fb[T::TN][decltype(sb)::PARTS];
 #pragma unroll
-    for (int i = 0; i < T::TM; ++i) sa.fragment(from, wm * T::TM + i, k, lane, fa[i]);
+    for (int i = 0; i < (int)(sizeof(fa) / sizeof(fa[0])); ++i) sa.fragment(from, wm * T::TM + i, k, lane, fa[i]);
 #pragma unroll
     for (int j = 0; j < T::TN; ++j) sb.fragment(from + B_AT, wn * T::TN + j, k, lane, fb[j]);
     __builtin_amdgcn_s_setprio(1);
-    multiply_parts<T::NP>(fa, fb, acc);
+    multiply_parts<T::NP>(fa, fb, part);
     __builtin_amdgcn_s_setprio(0);
+  };
+  // Cutting fp32 values costs as much as multiplying them: not done for blocks of 16 rows m that do not exist.
+  const int blocks = T::NP == 3 ? ((T::AX ? a.cols : a.rows) - m0 + 15) / 16 - wm * T::TM : T::TM;
+  const auto work = [&](const char* from, int k) {
+    if (T::NP < 3 || blocks > 1) {
+      u32x4 fa[T::TM][decltype(sa)::PARTS];
+      some(from, k, fa, acc);
+    } else if (blocks == 1) {
+      u32x4 fa[1][decltype(sa)::PARTS];
+      some(from, k, fa, reinterpret_cast<f32x4(&)[1][T::TN]>(acc));
+    }
   };
   const int stages = (k_end - k_begin) / T::K;
 #pragma unroll
