@@ -201,7 +201,7 @@ template <class T, int NP>
 __global__ __launch_bounds__(256) void k_loss_planes(Copy w, Copy h, unsigned first, Rows g) {
   __shared__ float lds[4];
   const bool of_w = blockIdx.x < first;
-  const Copy& o = of_w ? w : h;
+  const Copy o = of_w ? w : h;
   const unsigned block = of_w ? blockIdx.x : blockIdx.x - first, blocks = of_w ? first : gridDim.x - first;
   if (NP == 2 && !o.most) copy_rows_apart(o, block, blocks);
   else copy_rows<T, NP>(o, g, block, blocks, lds);

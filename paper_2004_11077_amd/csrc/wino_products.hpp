@@ -205,7 +205,8 @@ struct Side {
   int read[X ? 4 : 2];       // a lane's places in a stage
   int cols;
 
-  __device__ __forceinline__ Side(const Operand& o, long batch, int first, int k, int lane, int wave) {
+  // own: the wave's first block of 16 rows.
+  __device__ __forceinline__ Side(const Operand& o, long batch, int first, int k, int own, int lane, int wave) {
     const long start = X ? (long)k * o.ld + first * UNITS : (long)first * o.ld;
     base = o.p + batch * o.batch + start;
     if constexpr (X) {
@@ -240,7 +241,10 @@ struct Side {
     } else if constexpr (X) {
       const int g = lane >> 4, r = (lane >> 2) & 3, q = lane & 3, swap = swap_of(g * 8 + r);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) read[i] = g * 1024 + r * 128 + ((i * 2 + (q >> 1)) ^ swap) * 16 + (q & 1) * 8;
+      for (int i = 0; i < 4; ++i) {
+        const int place = NP == 1 ? (own + i) & 3 : i;   // one plane: of the wave's block i
+        read[i] = g * 1024 + r * 128 + ((place * 2 + (q >> 1)) ^ swap) * 16 + (q & 1) * 8;
+      }
     } else {
       const int r = lane & 7;
 #pragma unroll
@@ -262,9 +266,10 @@ struct Side {
     }
   }
 
-  // What the instruction takes of 16 rows `block` of the stage at k: the two parts of 32 k of one plane, the two
+  // What the instruction takes of 16 rows, block own + i, of the stage at k: the two parts of 32 k of one plane, the two
   // planes, or the three pieces of fp32 values.
-  __device__ __forceinline__ void fragment(const char* from, int block, int k, int lane, u32x4 (&out)[PARTS]) const {
+  __device__ __forceinline__ void fragment(const char* from, int own, int i, int k, int lane, u32x4 (&out)[PARTS]) const {
+    const int block = own + i;
     if constexpr (NP == 3) {
       f32x4 x[2];
       if constexpr (X) {
@@ -273,7 +278,7 @@ struct Side {
           x[j >> 2][j & 3] = *reinterpret_cast<const float*>(from + (block >> 1) * 4096 + j * 128 + read[(block & 1) * 2 + ((j >> 1) & 1)]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const f32x4*>(from + block * 2048 + read[i]);
+        for (int h = 0; h < 2; ++h) x[h] = *reinterpret_cast<const f32x4*>(from + block * 2048 + read[h]);
         if (k + 32 > cols)   // the next row's values, or nothing's
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -285,7 +290,7 @@ struct Side {
       for (int sub = 0; sub < 2; ++sub) {
         if constexpr (X) {
           typedef __attribute__((address_space(3))) s16x4 L;
-          const char* p = NP == 1 ? from + ((block >> 2) * 8 + sub * 4) * 1024 + read[block & 3]
+          const char* p = NP == 1 ? from + ((block >> 2) * 8 + sub * 4) * 1024 + read[i & 3]
                                   : from + (block >> 1) * 4096 + read[sub * 2 + (block & 1)];
           const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p));
           const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(p + 512)));
@@ -394,8 +399,8 @@ __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, lon
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % T::WM, wn = wave / T::WM;
   if (k_begin >= k_end) return;
-  Side<T::BM, T::AX, T::NP, T::NW> sa(a, batch, m0, k_begin, lane, wave);
-  Side<T::BN, T::BX, T::NP, T::NW> sb(b, batch, n0, k_begin, lane, wave);
+  Side<T::BM, T::AX, T::NP, T::NW> sa(a, batch, m0, k_begin, wm * T::TM, lane, wave);
+  Side<T::BN, T::BX, T::NP, T::NW> sb(b, batch, n0, k_begin, wn * T::TN, lane, wave);
   constexpr int B_AT = T::RA * 1024;
   const auto fetch = [&](int k, char* to) {
     sa.fetch(k, to, wave);
@@ -404,9 +409,9 @@ __device__ __forceinline__ void multiply(const Operand& a, const Operand& b, lon
   const auto some = [&](const char* from, int k, auto& fa, auto& part) {
     u32x4 fb[T::TN][decltype(sb)::PARTS];
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(fa) / sizeof(fa[0])); ++i) sa.fragment(from, wm * T::TM + i, k, lane, fa[i]);
+    for (int i = 0; i < (int)(sizeof(fa) / sizeof(fa[0])); ++i) sa.fragment(from, wm * T::TM, i, k, lane, fa[i]);
 #pragma unroll
-    for (int j = 0; j < T::TN; ++j) sb.fragment(from + B_AT, wn * T::TN + j, k, lane, fb[j]);
+    for (int j = 0; j < T::TN; ++j) sb.fragment(from + B_AT, wn * T::TN, j, k, lane, fb[j]);
     __builtin_amdgcn_s_setprio(1);
     multiply_parts<T::NP>(fa, fb, part);
     __builtin_amdgcn_s_setprio(0);
