@@ -502,9 +502,10 @@ hipError_t norm_backward(const NormArgs& a, const TG* dy, const TI* x, const flo
 }  // namespace
 
 int norm_parts(long rows, int channels) {
-  // Two work groups a compute unit; fewer for long rows, whose partial sums would be a large share
-  // of the traffic.
-  const long most = 512;
+  // Two work groups a compute unit.  Rows of more than 16384 values go by blocks of 256 columns too (the
+  // long form), so that fewer ranges of rows fill the chip, and the partial sums stay within 64 MiB up to
+  // 2^23 columns.
+  const long most = channels <= 16384 ? 512 : channels < 1 << 23 ? (512L << 14) / channels : 1;
   return (int)(rows < 1 ? 1 : rows < most ? rows : most);
 }
 

@@ -1,6 +1,5 @@
 // C ABI of the operators of a training step: argument checks and launches.
 #include <cmath>
-#include <cstring>
 
 #include "../../include/wino.h"
 #include "wino_kernels.hpp"

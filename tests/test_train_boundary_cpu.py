@@ -56,6 +56,14 @@ def test_norm_descriptors(i):
     assert binding._load().wino_layer_norm_backward_workspace_bytes(ref(d), C.byref(size)) == code
 
 
+def test_norm_workspace_stays_small():
+    """512 rows of partial sums up to 16384 channels, and no more bytes for longer rows until one row of
+    them is that long."""
+    for channels in (16, 16384, 16385, 100001, 1 << 20, 1 << 23, 1 << 24):
+        size = wn.wino_layer_norm_backward_workspace_bytes(wn.NormDesc(1 << 20, channels))
+        assert 8 * channels <= size <= max(8 * channels, 1 << 26)
+
+
 def test_norm_pointers():
     d = wn.NormDesc(3, 8, x_type=wn.TYPE_BF16, y_type=wn.TYPE_F32, g_type=wn.TYPE_F32)
     for kw in (dict(x=None), dict(y=None), dict(x=A + 1), dict(y=A + 2), dict(gamma=A + 2), dict(beta=A + 1), dict(mean=A + 2), dict(rstd=A + 3)):
