@@ -485,7 +485,8 @@ int wino_linear_cross_entropy_backward(const wino_loss_desc_t* d, const void* h,
  * NaN. */
 enum { WINO_ORTHOGONALISE_MAX_SIDE = 1 << 20 };
 typedef struct {
-  int batch, rows, cols;     /* batch at most 65535                             */
+  int batch, rows, cols;     /* batch at most 65535; in all at most 2^23 blocks of
+                                64 x 64, begun ones counted (EINVAL)            */
   int g_type, o_type;
   int steps;                 /* 1 ... 100                                       */
   float a, b, c, eps, scale; /* eps > 0                                         */

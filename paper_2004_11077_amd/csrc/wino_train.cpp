@@ -82,6 +82,9 @@ int update_args(const wino_orthogonalise_desc_t* d, UpdateArgs* a) {
   if (d->batch < 0 || d->batch > 65535) return refuse(WINO_EINVAL, "bad batch %d", d->batch);
   if (d->rows < 0 || d->cols < 0 || d->rows > WINO_ORTHOGONALISE_MAX_SIDE || d->cols > WINO_ORTHOGONALISE_MAX_SIDE)
     return refuse(WINO_EINVAL, "bad matrix %d x %d", d->rows, d->cols);
+  // a launch holds fewer than 2^32 threads, 256 a tile of 64 x 64
+  if ((int64_t)d->batch * ((d->rows + 63) / 64) * ((d->cols + 63) / 64) > 1 << 23)
+    return refuse(WINO_EINVAL, "%d matrices of %d x %d are too many", d->batch, d->rows, d->cols);
   if (!real_type(d->g_type) || !real_type(d->o_type))
     return refuse(WINO_EUNSUPPORTED, "%s", "g_type and o_type are WINO_TYPE_F32 or WINO_TYPE_BF16");
   if (d->steps < 1 || d->steps > 100) return refuse(WINO_EINVAL, "bad steps %d", d->steps);

@@ -128,7 +128,9 @@ UPDATE = [(None, EINVAL), (wn.OrthogonaliseDesc(-1, 4, 4), EINVAL), (wn.Orthogon
           (wn.OrthogonaliseDesc(1, 4, 4, a=NAN), EINVAL), (wn.OrthogonaliseDesc(1, 4, 4, c=INF), EINVAL),
           (wn.OrthogonaliseDesc(1, 4, 4, scale=NAN), EINVAL), (wn.OrthogonaliseDesc(1, 4, 4, eps=0), EINVAL),
           (wn.OrthogonaliseDesc(1, 4, 4, g_stride=3), EINVAL), (wn.OrthogonaliseDesc(1, 4, 4, o_stride=3), EINVAL),
-          (wn.OrthogonaliseDesc(2, 4, 4, g_batch=15), EINVAL), (wn.OrthogonaliseDesc(2, 4, 4, o_stride=6, o_batch=21), EINVAL)]
+          (wn.OrthogonaliseDesc(2, 4, 4, g_batch=15), EINVAL), (wn.OrthogonaliseDesc(2, 4, 4, o_stride=6, o_batch=21), EINVAL),
+          (wn.OrthogonaliseDesc(30000, 1, 1 << 20), EINVAL), (wn.OrthogonaliseDesc(1, 1 << 20, 1 << 20), EINVAL),
+          (wn.OrthogonaliseDesc(513, 1, 1 << 20), EINVAL)]
 
 
 @pytest.mark.parametrize("i", range(len(UPDATE)))
