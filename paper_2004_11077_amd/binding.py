@@ -559,11 +559,26 @@ def _fit(*tensors):
             raise WinoError(-1, "%s is not on the current device" % name)
 
 
+def _reach(*tensors):
+    """The same for rows that the descriptor lays a stride apart: (name, tensor or None, stride or 0,
+    rows, values of a row[, elements between matrices or 0, matrices])."""
+    for name, t, stride, rows, row, *more in tensors:
+        batch, count = more or (0, 1)
+        if t is None or not (stride or batch) or rows < 1 or row < 1 or count < 1:
+            continue
+        stride = stride or row
+        least = (rows - 1) * stride + row + (count - 1) * (batch or rows * stride)
+        have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if have < least:
+            raise WinoError(-1, "%s has %d elements to the end of its memory, its strides need %d" % (name, have, least))
+
+
 def wino_layer_norm(desc, x, gamma, beta, y, mean=None, rstd=None, stream=None):
     """Layer norm of the rows of ``x``; gamma, beta, mean and rstd may be None."""
     n, c = desc.rows, desc.channels
     _fit(("x", x, desc.x_type, n * c), ("gamma", gamma, TYPE_F32, c), ("beta", beta, TYPE_F32, c),
          ("y", y, desc.y_type, n * c), ("mean", mean, TYPE_F32, n), ("rstd", rstd, TYPE_F32, n))
+    _reach(("x", x, desc.x_stride, n, c), ("y", y, desc.y_stride, n, c))
     _check(_load().wino_layer_norm(C.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y),
                                    _ptr(mean), _ptr(rstd), _stream(stream)))
     return y
@@ -580,6 +595,7 @@ def wino_layer_norm_backward(desc, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, 
     _fit(("dy", dy, desc.g_type, n * c), ("x", x, desc.x_type, n * c), ("gamma", gamma, TYPE_F32, c),
          ("mean", mean, TYPE_F32, n), ("rstd", rstd, TYPE_F32, n), ("dx", dx, desc.g_type, n * c),
          ("dgamma", dgamma, TYPE_F32, c), ("dbeta", dbeta, TYPE_F32, c), ("workspace", workspace, None, 0))
+    _reach(("dy", dy, desc.dy_stride, n, c), ("x", x, desc.x_stride, n, c), ("dx", dx, desc.dx_stride, n, c))
     _check(_load().wino_layer_norm_backward(C.byref(desc), _ptr(dy), _ptr(x), _ptr(gamma),
                                             _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma),
                                             _ptr(dbeta), _ptr(workspace), _room(workspace),
@@ -597,6 +613,7 @@ def wino_linear_cross_entropy(desc, h, w, bias, targets, loss, lse, workspace, s
     _fit(("h", h, desc.type, t * d), ("w", w, desc.type, v * d if t else 0), ("bias", bias, TYPE_F32, v),
          ("targets", targets, "i64", t), ("loss", loss, TYPE_F32, t), ("lse", lse, TYPE_F32, t),
          ("workspace", workspace, None, 0))
+    _reach(("h", h, desc.h_stride, t, d), ("w", w, desc.w_stride, v if t else 0, d))
     _check(_load().wino_linear_cross_entropy(C.byref(desc), _ptr(h), _ptr(w), _ptr(bias),
                                              _ptr(targets), _ptr(loss), _ptr(lse), _ptr(workspace),
                                              _room(workspace), _stream(stream)))
@@ -615,6 +632,7 @@ def wino_linear_cross_entropy_backward(desc, h, w, bias, targets, lse, dloss, dh
          ("targets", targets, "i64", t), ("lse", lse, TYPE_F32, t), ("dloss", dloss, TYPE_F32, t),
          ("dh", dh, desc.type, t * d), ("dw", dw, desc.type, v * d), ("dbias", dbias, TYPE_F32, v),
          ("workspace", workspace, None, 0))
+    _reach(("h", h, desc.h_stride, t, d), ("w", w, desc.w_stride, v if t else 0, d))
     _check(_load().wino_linear_cross_entropy_backward(
         C.byref(desc), _ptr(h), _ptr(w), _ptr(bias), _ptr(targets), _ptr(lse), _ptr(dloss),
         _ptr(dh), _ptr(dw), _ptr(dbias), _ptr(workspace), _room(workspace), _stream(stream)))
@@ -629,6 +647,8 @@ def wino_orthogonalise(desc, g, o, workspace, stream=None):
     """Orthogonalised updates of a batch of weight gradients."""
     n = desc.batch * desc.rows * desc.cols
     _fit(("g", g, desc.g_type, n), ("o", o, desc.o_type, n), ("workspace", workspace, None, 0))
+    _reach(("g", g, desc.g_stride, desc.rows, desc.cols, desc.g_batch, desc.batch),
+           ("o", o, desc.o_stride, desc.rows, desc.cols, desc.o_batch, desc.batch))
     _check(_load().wino_orthogonalise(C.byref(desc), _ptr(g), _ptr(o), _ptr(workspace),
                                       _room(workspace), _stream(stream)))
     return o

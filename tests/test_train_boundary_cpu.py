@@ -156,3 +156,16 @@ def test_errors_name_the_argument():
         wn.wino_orthogonalise_workspace_bytes(wn.OrthogonaliseDesc(1, 4, 4, steps=0))
     with pytest.raises(wn.WinoError, match="classes"):
         wn.wino_linear_cross_entropy_workspace_bytes(wn.LossDesc(1, 4, 0))
+
+
+def test_strides_reach_within_the_tensor():
+    torch = pytest.importorskip("torch")
+    whole = torch.zeros(100)
+    binding._reach(("x", whole[10:], 9, 10, 9), ("y", None, 100, 10, 9), ("z", whole, 0, 1000, 1000),
+                   ("none", whole, 50, 0, 50), ("view", whole.view(10, 10)[:, :3], 10, 10, 3),
+                   ("g", whole, 10, 2, 7, 41, 3), ("dense rows", whole, 0, 5, 4, 40, 3), ("one", whole, 0, 4, 5, 0, 3))
+    for bad in (("x", whole[11:], 9, 10, 9), ("view", whole.view(10, 10)[:, 3:], 10, 10, 8),
+                ("g", whole, 10, 2, 7, 42, 3), ("rows", whole, 0, 5, 4, 41, 3), ("stride", whole, 10, 4, 7, 0, 3)):
+        with pytest.raises(wn.WinoError) as e:
+            binding._reach(bad)
+        assert e.value.code == EINVAL and bad[0] in str(e.value)
