@@ -17,7 +17,7 @@
  *   Every device tensor must start on a 16-byte boundary (EINVAL otherwise),
  *   except that the fp32 path (bits_in = 32) takes its tensors at any float and
  *   the flex calls take x, w and y, the flex stage transforms also U, V and M,
- *   at any element.
+ *   and the operators of a training step all their tensors, at any element.
  *
  * Every function returns WINO_OK (0) or a negative error code and never
  * throws or aborts; wino_last_error() gives the text of the last failure on
@@ -444,7 +444,7 @@ int wino_layer_norm_backward(const wino_norm_desc_t* d, const void* dy, const vo
  * be masked by a bias of -infinity: a masked target's loss is +infinity; a row
  * with every class masked has lse -infinity, loss +infinity and no gradient.
  * Products of fp32 operands take 22 bits of each factor (of values below 2^-18
- * of the tensor's largest: 2^-39 of that), for 64 rows or fewer and 2^22 weights
+ * of the tensor's largest: 2^-39 of that), for 192 rows or fewer and 2^16 weights
  * or more 24 bits (of values above 2^-102), and sum in fp32. */
 enum { WINO_LOSS_MAX_ROWS = 1 << 21, WINO_LOSS_MAX_FEATURES = 1 << 20, WINO_LOSS_MAX_CLASSES = 1 << 27 };
 typedef struct {

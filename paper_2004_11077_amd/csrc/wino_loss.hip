@@ -3,6 +3,14 @@
 //   l = h W^T + b,  lse_t = log sum_v exp(l_tv),  loss_t = lse_t - l_t[target_t]
 //   dl_tv = (exp(l_tv - lse_t) - [v = target_t]) dloss_t,  dh = dl W,  dW = dl^T h,  db = sum_t dl
 //
+// What bounds it: the matrix pipe, 8 T D V operations for a training step of T rows, D features and V
+// classes (the logits are computed twice).  T = 4096, D = 2048, V = 65536 in bf16: 4.0 ms, 1.1 PFLOP/s, the
+// library's large product at 8192^3 reaching 1.3; 1001 x 515 x 10007 in fp32 on two planes: 266 us, 155
+// TFLOP/s of fp32 (465 of the matrix pipe's, tiles that are not full and the planes' copies are the rest).
+// Few rows: the weights' passage through memory.  One row of 4096 x 131072 in bf16: 176 us, 6.1 TB/s; a
+// training step of 3 x 925 x 75113 in fp32: 326 us, of which 160 read W and write dW.  Small ones: launches,
+// 256 x 512 x 10: eight in 36 us.
+//
 // Forward: the logits of a tile leave the matrix instructions in registers and end there as a maximum
 // and a sum of exponentials a row; those of all tiles are joined by a second kernel.  Backward: the
 // logits are computed again, piece by piece of the classes, and become dl in the workspace, the
@@ -35,7 +43,6 @@ constexpr float kInf = __builtin_inff();
 struct Numbers {
   float ref;              // largest |dloss|
   int of_w, of_h;         // exponents of W's, h's planes: they hold 2^e times the values
-  int pad;
   float max_w[kRange], max_h[kRange];
 };
 
@@ -517,7 +524,8 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_product(Product p) {
   __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
   make_product<T, FOUR>(p, blockIdx.x, gridDim.x, blockIdx.y, lds);
 }
-// dh and dW of a piece in one launch, where both have few tiles: the first `first` work groups have dh's
+// dh and dW of a piece in one launch, where both have few tiles and would each leave compute units idle
+// (2048 x 64 x 1000 in fp32, a training step: 63 us, with two launches 70; 59 x 4081 x 25462: 582 and 609): the first `first` work groups have dh's
 // tiles and ranges, the others dW's.
 template <class H, class W>
 __global__ __launch_bounds__(H::THREADS) void k_loss_products(Product h, Product w, int first, int tiles_h,
@@ -574,10 +582,12 @@ struct Tiles {
   typedef Tile<64, 64, 2, 2, NP, 2, AX, BX> Small;
   typedef Tile<64, 64, 2, 2, NP, 4, AX, BX> Deep;   // where two work groups a compute unit are all there are
 };
+// (A training step of 900 x 4092 x 401 in bf16: 104 us, all of ring 2 125; of 3 x 925 x 75113 in fp32: 328, all of
+// ring 4 428.)
 constexpr long kDeepGroups = 512;
 long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
 // Products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the waves where
-// there are few tiles.
+// there are few tiles.  (A training step of 64 x 512 x 2048 in fp32: 56 us, with tiles of 64 62.)
 int least_side(long m, long n, long k) { return count_of(m, n, 64) < 64 && k >= 256 ? 32 : 64; }
 int side_along(long m, long n, long k) {
   const int side = side_for(m, n, 1);
@@ -603,10 +613,12 @@ bool direct(const LossArgs& a, const void* p, long stride) {
 }
 
 // fp32 as it stands: few rows, where the time is W's passage through memory (75113 x 925 and 3 rows, a
-// training step: 951 us by way of planes).  Values below 2^-102 lose lower pieces to bf16's smallest
-// numbers there, so smaller weights keep to the planes.
+// training step: 326 us, by way of planes 821; 192 rows 907 and 1149, 256 rows 1160 and 1237; 256 x 1024 x
+// 8192, where every tile of W is cut four times: 151 and 143; 44 x 1452 x 2481: 70 and 97).  Values below 2^-102
+// lose lower pieces to bf16's smallest numbers there, which planes keep, so small weights, where the gain is
+// a few microseconds of launches (64 x 64 x 1000: 42.3 us and 45.2), stay with the planes.
 bool as_it_stands(const LossArgs& a) {
-  return !a.bf16 && a.rows <= 64 && (double)a.features * a.classes >= 1 << 22 && a.h_stride <= kMaxLd / 2 &&
+  return !a.bf16 && a.rows <= 192 && (double)a.features * a.classes >= 1 << 16 && a.h_stride <= kMaxLd / 2 &&
          a.w_stride <= kMaxLd / 2;
 }
 
@@ -826,7 +838,8 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
     }
     if (l.splits > 64) l.splits = 64;   // k_loss_sums adds them up one after the other
     l.dh = take(4 * T * D * l.splits);
-    // ranges of rows, each of 256 or more, where dW has few tiles of 64
+    // ranges of rows, each of 256 or more, where dW has few tiles of 64 (a training step of 2048 x 64 x 1000 in
+    // fp32: 63 us, without them 87)
     const long tiles = count_of((long)P, (long)D, 64);
     long ranges = tiles < 128 ? 256 / tiles : 1;
     if (ranges > (long)T / 256) ranges = (long)T / 256;

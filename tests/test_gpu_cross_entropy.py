@@ -152,6 +152,13 @@ def test_few_rows_beside_rows_left_out():
     check(r, "f32")
 
 
+@pytest.mark.parametrize("T", [2, 16, 17, 33, 48, 65, 100, 192, 193])
+@pytest.mark.parametrize("D,V", [(67, 1000), (256, 257), (512, 1040)])
+def test_rows_up_to_where_weights_are_copied(T, D, V):
+    """Rows that leave out some of a tile's blocks and waves, and the first number of rows that takes planes."""
+    check(run(T, D, V, "f32", extra=1), "f32")
+
+
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 def test_split_classes(type):
     """Few tiles of dh and many classes: ranges of classes are summed apart."""
