@@ -445,7 +445,8 @@ int wino_layer_norm_backward(const wino_norm_desc_t* d, const void* dy, const vo
  * with every class masked has lse -infinity, loss +infinity and no gradient.
  * Products of fp32 operands take 22 bits of each factor (of values below 2^-18
  * of the tensor's largest: 2^-39 of that), for 192 rows or fewer and 2^16 weights
- * or more 24 bits (of values above 2^-102), and sum in fp32. */
+ * or more, and for 64 classes or fewer and 2^16 values of h or more, 24 bits (of
+ * values above 2^-102), and sum in fp32. */
 enum { WINO_LOSS_MAX_ROWS = 1 << 21, WINO_LOSS_MAX_FEATURES = 1 << 20, WINO_LOSS_MAX_CLASSES = 1 << 27 };
 typedef struct {
   int rows, features, classes;

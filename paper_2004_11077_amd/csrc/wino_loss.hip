@@ -587,11 +587,18 @@ struct Tiles {
 constexpr long kDeepGroups = 512;
 long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
 // Products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the waves where
-// there are few tiles.  (A training step of 64 x 512 x 2048 in fp32: 56 us, with tiles of 64 62.)
-int least_side(long m, long n, long k) { return count_of(m, n, 64) < 64 && k >= 256 ? 32 : 64; }
-int side_along(long m, long n, long k) {
+// there are few tiles, which for fp32, three or six products a term, are more, and more again where half
+// of a tile of 64 or more would be empty.  (Training steps: 64 x 512 x 2048 in fp32 56 us, with tiles of 64 62;
+// 4330 x 3610 x 8, 68 tiles: 178 and 251; 4096 x 2048 x 128, 128 tiles: 191 and 169; 3 x 925 x 10000, 157 tiles: 67
+// and 95; 900 x 4092 x 401 in bf16, 105 tiles: 128 and 104.)
+constexpr long few_tiles(bool bf16) { return bf16 ? 64 : 128; }
+int least_side(bool bf16, long m, long n, long k) {
+  const long few = !bf16 && (m <= 32 || n <= 32) ? 256 : few_tiles(bf16);
+  return count_of(m, n, 64) < few && k >= 256 ? 32 : 64;
+}
+int side_along(bool bf16, long m, long n, long k) {
   const int side = side_for(m, n, 1);
-  return side == 64 ? least_side(m, n, k) : side;
+  return side == 64 ? least_side(bf16, m, n, k) : side;
 }
 constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
 
@@ -612,14 +619,16 @@ bool direct(const LossArgs& a, const void* p, long stride) {
   return a.bf16 && a.features % 64 == 0 && stride % 8 == 0 && stride <= kMaxLd && ((uintptr_t)p & 15) == 0;
 }
 
-// fp32 as it stands: few rows, where the time is W's passage through memory (75113 x 925 and 3 rows, a
+// fp32 as it stands: few rows or classes, where the time is the passage of W or h through memory (75113 x 925 and 3 rows, a
 // training step: 326 us, by way of planes 821; 192 rows 907 and 1149, 256 rows 1160 and 1237; 256 x 1024 x
-// 8192, where every tile of W is cut four times: 151 and 143; 44 x 1452 x 2481: 70 and 97).  Values below 2^-102
-// lose lower pieces to bf16's smallest numbers there, which planes keep, so small weights, where the gain is
+// 8192, where every tile of W is cut four times: 151 and 143; 44 x 1452 x 2481: 70 and 97; 20000 x 1030 x 3: 228 and 299; 4096 x 2048 x 128: 197 and 169).  Values below 2^-102
+// lose lower pieces to bf16's smallest numbers there, which planes keep, so small tensors, where the gain is
 // a few microseconds of launches (64 x 64 x 1000: 42.3 us and 45.2), stay with the planes.
 bool as_it_stands(const LossArgs& a) {
-  return !a.bf16 && a.rows <= 192 && (double)a.features * a.classes >= 1 << 16 && a.h_stride <= kMaxLd / 2 &&
-         a.w_stride <= kMaxLd / 2;
+  const double least = 1 << 16;
+  return !a.bf16 && a.h_stride <= kMaxLd / 2 && a.w_stride <= kMaxLd / 2 &&
+         ((a.rows <= 192 && (double)a.features * a.classes >= least) ||
+          (a.classes <= 64 && (double)a.features * a.rows >= least));
 }
 
 const void* row_at(const LossArgs& a, const void* p, long row, long stride) {
@@ -676,7 +685,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
     q.count = (int)(a.classes - first < piece ? a.classes - first : piece);
     operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, num, ws, &ow, &oh, st);
     h_ready = true;
-    with_tile<NP, false, false>(NP == 3 ? least_side(q.count, a.rows, l.dp) : side_along(q.count, a.rows, l.dp),
+    with_tile<NP, false, false>(NP == 3 ? least_side(false, q.count, a.rows, l.dp) : side_along(a.bf16, q.count, a.rows, l.dp),
                                 count_of(q.count, a.rows, 64), [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
@@ -812,7 +821,8 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
   l.splits = 1;
   if (!back) {
     // pieces are whole multiples of 256 classes, so no tile spans two
-    const size_t least = T >= 64 * 64 ? 64 : 32;   // of side_along() for any classes
+    // of side_along() for any classes (32 or fewer are one tile of either side)
+    const size_t least = T >= 64 * (size_t)few_tiles(a.bf16) ? 64 : 32;
     l.parts = take(8 * T * (up(V, 256) / least));
     l.target = take(4 * T);
     l.unit_w = take(4 * P);
@@ -824,7 +834,7 @@ LossLayout loss_layout(const LossArgs& a, bool back) {
     l.two = a.bf16 && (T <= 64 || (double)T * D * V <= 1 << 30);
     if (l.two) l.rest = take(item * T * vp);
     const bool stands = as_it_stands(a);
-    l.side = stands ? least_side((long)P, (long)T, l.dp) : side_along((long)P, (long)T, l.dp);
+    l.side = stands ? least_side(false, (long)P, (long)T, l.dp) : side_along(a.bf16, (long)P, (long)T, l.dp);
     // ranges of classes, each of 512 or more, until dh's tiles fill the chip: one tile of 256 a compute
     // unit, or two of the smaller ones
     const long room = (long)(vp / 512 ? vp / 512 : 1);

@@ -159,6 +159,17 @@ def test_rows_up_to_where_weights_are_copied(T, D, V):
     check(run(T, D, V, "f32", extra=1), "f32")
 
 
+@pytest.mark.parametrize("T,D,V", [(1000, 67, 3), (300, 520, 10), (4099, 300, 64), (8300, 257, 1), (17000, 260, 32), (16400, 256, 33), (1030, 64, 65)])
+def test_few_classes_and_many_rows(T, D, V):
+    check(run(T, D, V, "f32", extra=3), "f32")
+
+
+@pytest.mark.parametrize("T,D,V", [(4097, 256, 200), (8000, 256, 66), (2, 300, 16000), (40, 256, 8100)])
+def test_products_of_few_tiles(T, D, V):
+    """About as many tiles as k is shared between a work group's waves for."""
+    check(run(T, D, V, "f32"), "f32")
+
+
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 def test_split_classes(type):
     """Few tiles of dh and many classes: ranges of classes are summed apart."""
