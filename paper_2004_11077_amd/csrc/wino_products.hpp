@@ -11,7 +11,8 @@
 // block of 32 k costs three roundings of the sum and not 32), at three matrix instructions of 2.5
 // PFLOP/s instead of one fp32 instruction of 0.157 PFLOP/s.  NP = 3: fp32 values as they stand, cut into
 // three bf16 values of 8 bits each when they are read from LDS, and six of nine products: twice the
-// instructions and the cutting for every tile, but no planes to be written and read and no power of two
+// instructions and the cutting for every tile (as many cycles again: 59 x 4081 x 25462 takes 179 us where its
+// 416 MB would pass in 86), but no planes to be written and read and no power of two
 // to be known.  It is for operands that are read about once.
 //
 // Two planes lie together, 32 elements of the one and then 32 of the other: 128 bytes, a cache line.
