@@ -219,7 +219,7 @@ struct Logits {
   const float* bias;         // of all classes, may be null
   Rows g;
   int first, count;          // classes of this piece
-  int k;                     // features in whole blocks
+  int k;                     // features in whole stages
   const int* of_w;           // fp32: the planes' exponents, one for all rows or (apart) one a row
   const int* of_h;
   int apart;
@@ -635,6 +635,11 @@ const void* row_at(const LossArgs& a, const void* p, long row, long stride) {
   return static_cast<const char*>(p) + row * stride * (a.bf16 ? 2 : 4);
 }
 
+// What k of the logits runs to: rows of planes are padded to whole lines of 64 or two of 32, tensors that are
+// read as they stand are not, and no stage may lie behind their rows.
+template <int NP>
+int logits_k(const LossArgs& a, const LossLayout& l) { return NP == 3 ? whole_stages_of_32(a.features) : l.dp; }
+
 // Operands of a piece: where they lie, or planes made here.
 template <int NP>
 void operands(const LossArgs& a, const LossLayout& l, const Rows& g, const void* w_rows, int count, const void* h,
@@ -678,7 +683,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
   const long most = (1L << 21) / ((a.rows + 63) / 64) * 64;
   long piece = w_direct || NP == 3 ? a.classes : l.piece;
   if (piece > most) piece = most < 256 ? 256 : most / 256 * 256;
-  Logits q{bias, g, 0, 0, l.dp, reinterpret_cast<const int*>(ws + l.unit_w), reinterpret_cast<const int*>(ws + l.unit_h), 1};
+  Logits q{bias, g, 0, 0, logits_k<NP>(a, l), reinterpret_cast<const int*>(ws + l.unit_w), reinterpret_cast<const int*>(ws + l.unit_h), 1};
   int part = 0;
   for (long first = 0; first < a.classes; first += piece) {
     q.first = (int)first;
@@ -720,7 +725,7 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
   const bool w_direct = direct(a, w, a.w_stride);
   bool h_ready = false;   // always a copy: rows that are left out as zeros
   Operand oh{}, ow{};
-  Logits q{bias, g, 0, 0, l.dp, &num->of_w, &num->of_h, 0};
+  Logits q{bias, g, 0, 0, logits_k<NP>(a, l), &num->of_w, &num->of_h, 0};
   uint16_t* dl = reinterpret_cast<uint16_t*>(ws + l.dl);
   uint16_t* rest = l.two ? reinterpret_cast<uint16_t*>(ws + l.rest) : nullptr;
   float* db = dbias ? reinterpret_cast<float*>(ws + l.dbias) : nullptr;

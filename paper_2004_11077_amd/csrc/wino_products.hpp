@@ -31,7 +31,8 @@
 // waits until its own copies of a stage have landed (counted, so that the later stages' stay under
 // way), the barrier then says so of all waves, and also that the buffer of the stage before may be
 // filled again.  What lies outside an operand lies outside its buffer descriptor and reads as zeros; k
-// runs in whole stages: along rows the caller pads with zeros.  A work group's first row exists, and
+// runs in whole stages: along rows the caller pads with zeros, but for fp32 values as they stand, whose
+// last stage may be a part of one (wino_product_sources.hpp).  A work group's first row exists, and
 // kMaxLd bounds the offsets within a stage to 31 bits.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -39,6 +40,7 @@
 #include <cstdint>
 
 #include "wino_kernels.hpp"
+#include "wino_product_sources.hpp"
 
 namespace wino {
 namespace prod {
@@ -204,7 +206,7 @@ struct Side {
   __amdgpu_buffer_rsrc_t rsrc;
   int at[N];                 // a copy's source, in bytes from the base
   int read[X ? 4 : 2];       // a lane's places in a stage
-  int cols;
+  int cols, value;           // value: fp32 along rows, the stage's k that the lane copies from
 
   // own: the wave's first block of 16 rows.
   __device__ __forceinline__ Side(const Operand& o, long batch, int first, int k, int own, int lane, int wave) {
@@ -233,6 +235,7 @@ struct Side {
       }
     }
     cols = o.cols;
+    value = copied_value(lane);
     if constexpr (X && NP == 3) {
       // place i: half i / 2 of 32 values, rows with bit 1 of k as i % 2
       const int g = lane >> 4, e = lane & 15;
@@ -257,10 +260,17 @@ struct Side {
   // Copies the stage at k (the next one, for k across) to LDS.
   __device__ __forceinline__ void fetch(int k, char* to, int wave) {
     if constexpr (X) rsrc = window(base, bytes);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
+    const auto copy = [&](int i, int lane_at, int scalar_at) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rsrc, (__attribute__((address_space(3))) void*)(to + (i * NW + wave) * 1024), 16, at[i], X ? 0 : k * 2 * UNITS, 0, 0);
+          rsrc, (__attribute__((address_space(3))) void*)(to + (i * NW + wave) * 1024), 16, lane_at, scalar_at, 0, 0);
+    };
+    if (NP == 3 && !X && k + K > cols) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) copy(i, source_at(at[i], value, k, cols).lane, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) copy(i, at[i], X ? 0 : k * 2 * UNITS);
+    }
     if constexpr (X) {
       base += step;
       bytes -= step * 2;
@@ -341,14 +351,18 @@ __device__ __forceinline__ void multiply_few(const Operand& a, const Operand& b,
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
       // lines beyond the last one: out of the window, zeros
-      const int line = l + d * T::WAVES, off = line < lines ? 0 : 0x40000000;
+      const int line = l + d * T::WAVES;
+      const auto load = [&](auto rsrc, int at, int cols, int q) {
+        Source s{kRefused, 0};
+        if (line < lines) s = T::NP == 3 ? source_at(at, loaded_value(lane, q), line * 32, cols) : Source{at, line * 128};
+        return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, s.lane, s.scalar, 0));
+      };
 #pragma unroll
       for (int q = 0; q < 2; ++q)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int to = off ? 0 : line * 128;
-          fa[d][i][q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, (at_a + i * next_a + q * HALF) | off, to, 0));
-          fb[d][i][q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rb, (at_b + i * next_b + q * HALF) | off, to, 0));
+          fa[d][i][q] = load(ra, at_a + i * next_a + q * HALF, a.cols, q);
+          fb[d][i][q] = load(rb, at_b + i * next_b + q * HALF, b.cols, q);
         }
     }
     __builtin_amdgcn_sched_barrier(0);   // all loads before the first product
