@@ -538,47 +538,104 @@ def _room(workspace):
 _types = None
 
 
-def _fit(*tensors):
-    """Refuses tensors that a kernel would read or write past their end, or on another device than
-    the current one: (name, tensor or None, TYPE_* or a torch type, least number of elements)."""
+def _known_types():
     global _types
-    if _types is None:
-        import torch
-        _types = (torch.cuda.current_device, {TYPE_F32: torch.float32, TYPE_BF16: torch.bfloat16,
-                                              TYPE_I8: torch.int8, "i64": torch.int64})
-    device = _types[0]()
+    import torch
+    torch.cuda.init()
+    device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _types = (device, {TYPE_F32: torch.float32, TYPE_BF16: torch.bfloat16, TYPE_I8: torch.int8, "i64": torch.int64})
+    return _types
+
+
+def _fit(*tensors):
+    """Refuses tensors that are not what a kernel takes them for: (name, tensor or None, TYPE_* or torch type or None
+    for any, least number of elements).  They are of that type, on the current device and contiguous, so that as
+    many elements lie in memory as the shape says: an expanded tensor has fewer, and autograd's gradient at the losses
+    of a mean is one, one element seen as many."""
+    current, types = _types or _known_types()
+    device = current()
     for name, t, kind, least in tensors:
         if t is None:
             continue
-        dtype = _types[1].get(kind)
-        if dtype is not None and t.dtype is not dtype:      # an unknown type is the library's to refuse
-            raise WinoError(-1, "%s is %s, the descriptor says %s" % (name, t.dtype, dtype))
-        if t.numel() < least:
-            raise WinoError(-1, "%s has %d elements, %d needed" % (name, t.numel(), least))
-        if t.get_device() != device:
-            raise WinoError(-1, "%s is not on the current device" % name)
+        whole = t.is_contiguous()
+        if not whole or t.dtype is not types.get(kind) or t.numel() < least or t.get_device() != device:
+            _refuse(name, t, types.get(kind), least, device, whole)
+
+
+def _refuse(name, t, dtype, least, device, whole=True):
+    if not whole:
+        raise WinoError(-1, "%s is not contiguous" % name)
+    if t.dtype is not dtype and dtype is not None:      # an unknown type is the library's to refuse
+        raise WinoError(-1, "%s is %s, the descriptor says %s" % (name, t.dtype, dtype))
+    if t.numel() < least:
+        raise WinoError(-1, "%s has %d elements, %d needed" % (name, t.numel(), least))
+    if t.get_device() != device:
+        raise WinoError(-1, "%s is not on the current device" % name)
+
+
+def _fit_rows(*tensors):
+    """The same for tensors whose rows the descriptor may lay a stride apart: (name, tensor or None, type, stride or 0,
+    rows, values of a row[, elements between matrices or 0, matrices])."""
+    current, types = _types or _known_types()
+    device = current()
+    for name, t, kind, stride, rows, row, *more in tensors:
+        if t is None:
+            continue
+        if stride or more or not t.is_contiguous():
+            _reach((name, t, stride, rows, row, *more))
+        least = rows * row * more[1] if more else rows * row
+        if t.dtype is not types.get(kind) or t.numel() < least or t.get_device() != device:
+            _refuse(name, t, types.get(kind), least, device)
+
+
+def _blocks(levels):
+    """(elements, elements apart) from the innermost level on; a level that continues the one below joins it."""
+    out = [(1, 1)]
+    for size, apart in levels:
+        if size == 1:
+            continue
+        inner, below = out[-1]
+        if apart == inner * below:
+            out[-1] = (inner * size, below)
+        else:
+            out.append((size, apart))
+    return out
 
 
 def _reach(*tensors):
-    """The same for rows that the descriptor lays a stride apart: (name, tensor or None, stride or 0,
-    rows, values of a row[, elements between matrices or 0, matrices])."""
+    """Refuses tensors whose elements do not lie where the descriptor has them, or whose memory ends before: (name,
+    tensor or None, stride or 0, rows, values of a row[, elements between matrices or 0, matrices]).  Without a
+    stride they are contiguous; with one they lie so far apart, or are one run of memory that the strides cut up."""
     for name, t, stride, rows, row, *more in tensors:
         batch, count = more or (0, 1)
-        if t is None or not (stride or batch) or rows < 1 or row < 1 or count < 1:
+        if t is None or rows < 1 or row < 1 or count < 1:
+            continue
+        whole = t.is_contiguous()
+        if not (stride or batch):
+            if not whole:
+                raise WinoError(-1, "%s is not contiguous, and the descriptor has no stride for it" % name)
             continue
         stride = stride or row
-        least = (rows - 1) * stride + row + (count - 1) * (batch or rows * stride)
+        batch = batch or rows * stride
+        least = (rows - 1) * stride + row + (count - 1) * batch
         have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
         if have < least:
             raise WinoError(-1, "%s has %d elements to the end of its memory, its strides need %d" % (name, have, least))
+        if whole and t.numel() >= least:
+            continue
+        want = _blocks([(row, 1), (rows, stride), (count, batch)])
+        laid = _blocks(list(zip(t.shape, t.stride()))[::-1])[:len(want)]
+        if ([apart for _, apart in laid] != [apart for _, apart in want] or laid[:-1] != want[:-1] or
+                laid[-1][0] < want[-1][0]):
+            raise WinoError(-1, "%s has strides %s, the descriptor has rows %d apart" % (name, tuple(t.stride()), stride))
 
 
 def wino_layer_norm(desc, x, gamma, beta, y, mean=None, rstd=None, stream=None):
     """Layer norm of the rows of ``x``; gamma, beta, mean and rstd may be None."""
     n, c = desc.rows, desc.channels
-    _fit(("x", x, desc.x_type, n * c), ("gamma", gamma, TYPE_F32, c), ("beta", beta, TYPE_F32, c),
-         ("y", y, desc.y_type, n * c), ("mean", mean, TYPE_F32, n), ("rstd", rstd, TYPE_F32, n))
-    _reach(("x", x, desc.x_stride, n, c), ("y", y, desc.y_stride, n, c))
+    _fit_rows(("x", x, desc.x_type, desc.x_stride, n, c), ("y", y, desc.y_type, desc.y_stride, n, c))
+    _fit(("gamma", gamma, TYPE_F32, c), ("beta", beta, TYPE_F32, c), ("mean", mean, TYPE_F32, n),
+         ("rstd", rstd, TYPE_F32, n))
     _check(_load().wino_layer_norm(C.byref(desc), _ptr(x), _ptr(gamma), _ptr(beta), _ptr(y),
                                    _ptr(mean), _ptr(rstd), _stream(stream)))
     return y
@@ -592,10 +649,10 @@ def wino_layer_norm_backward(desc, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, 
                              stream=None):
     """Gradients of wino_layer_norm; each of dx, dgamma and dbeta may be None."""
     n, c = desc.rows, desc.channels
-    _fit(("dy", dy, desc.g_type, n * c), ("x", x, desc.x_type, n * c), ("gamma", gamma, TYPE_F32, c),
-         ("mean", mean, TYPE_F32, n), ("rstd", rstd, TYPE_F32, n), ("dx", dx, desc.g_type, n * c),
+    _fit_rows(("dy", dy, desc.g_type, desc.dy_stride, n, c), ("x", x, desc.x_type, desc.x_stride, n, c),
+              ("dx", dx, desc.g_type, desc.dx_stride, n, c))
+    _fit(("gamma", gamma, TYPE_F32, c), ("mean", mean, TYPE_F32, n), ("rstd", rstd, TYPE_F32, n),
          ("dgamma", dgamma, TYPE_F32, c), ("dbeta", dbeta, TYPE_F32, c), ("workspace", workspace, None, 0))
-    _reach(("dy", dy, desc.dy_stride, n, c), ("x", x, desc.x_stride, n, c), ("dx", dx, desc.dx_stride, n, c))
     _check(_load().wino_layer_norm_backward(C.byref(desc), _ptr(dy), _ptr(x), _ptr(gamma),
                                             _ptr(mean), _ptr(rstd), _ptr(dx), _ptr(dgamma),
                                             _ptr(dbeta), _ptr(workspace), _room(workspace),
@@ -610,10 +667,9 @@ def wino_linear_cross_entropy_workspace_bytes(desc):
 def wino_linear_cross_entropy(desc, h, w, bias, targets, loss, lse, workspace, stream=None):
     """Loss and log-sum-exp of every row; bias may be None, targets are int64."""
     t, d, v = desc.rows, desc.features, desc.classes
-    _fit(("h", h, desc.type, t * d), ("w", w, desc.type, v * d if t else 0), ("bias", bias, TYPE_F32, v),
-         ("targets", targets, "i64", t), ("loss", loss, TYPE_F32, t), ("lse", lse, TYPE_F32, t),
-         ("workspace", workspace, None, 0))
-    _reach(("h", h, desc.h_stride, t, d), ("w", w, desc.w_stride, v if t else 0, d))
+    _fit_rows(("h", h, desc.type, desc.h_stride, t, d), ("w", w, desc.type, desc.w_stride, v if t else 0, d))
+    _fit(("bias", bias, TYPE_F32, v), ("targets", targets, "i64", t), ("loss", loss, TYPE_F32, t),
+         ("lse", lse, TYPE_F32, t), ("workspace", workspace, None, 0))
     _check(_load().wino_linear_cross_entropy(C.byref(desc), _ptr(h), _ptr(w), _ptr(bias),
                                              _ptr(targets), _ptr(loss), _ptr(lse), _ptr(workspace),
                                              _room(workspace), _stream(stream)))
@@ -628,11 +684,10 @@ def wino_linear_cross_entropy_backward(desc, h, w, bias, targets, lse, dloss, dh
                                        workspace, stream=None):
     """Gradients of wino_linear_cross_entropy; each of dh, dw and dbias may be None."""
     t, d, v = desc.rows, desc.features, desc.classes
-    _fit(("h", h, desc.type, t * d), ("w", w, desc.type, v * d if t else 0), ("bias", bias, TYPE_F32, v),
-         ("targets", targets, "i64", t), ("lse", lse, TYPE_F32, t), ("dloss", dloss, TYPE_F32, t),
-         ("dh", dh, desc.type, t * d), ("dw", dw, desc.type, v * d), ("dbias", dbias, TYPE_F32, v),
-         ("workspace", workspace, None, 0))
-    _reach(("h", h, desc.h_stride, t, d), ("w", w, desc.w_stride, v if t else 0, d))
+    _fit_rows(("h", h, desc.type, desc.h_stride, t, d), ("w", w, desc.type, desc.w_stride, v if t else 0, d))
+    _fit(("bias", bias, TYPE_F32, v), ("targets", targets, "i64", t), ("lse", lse, TYPE_F32, t),
+         ("dloss", dloss, TYPE_F32, t), ("dh", dh, desc.type, t * d), ("dw", dw, desc.type, v * d),
+         ("dbias", dbias, TYPE_F32, v), ("workspace", workspace, None, 0))
     _check(_load().wino_linear_cross_entropy_backward(
         C.byref(desc), _ptr(h), _ptr(w), _ptr(bias), _ptr(targets), _ptr(lse), _ptr(dloss),
         _ptr(dh), _ptr(dw), _ptr(dbias), _ptr(workspace), _room(workspace), _stream(stream)))
@@ -645,10 +700,9 @@ def wino_orthogonalise_workspace_bytes(desc):
 
 def wino_orthogonalise(desc, g, o, workspace, stream=None):
     """Orthogonalised updates of a batch of weight gradients."""
-    n = desc.batch * desc.rows * desc.cols
-    _fit(("g", g, desc.g_type, n), ("o", o, desc.o_type, n), ("workspace", workspace, None, 0))
-    _reach(("g", g, desc.g_stride, desc.rows, desc.cols, desc.g_batch, desc.batch),
-           ("o", o, desc.o_stride, desc.rows, desc.cols, desc.o_batch, desc.batch))
+    _fit_rows(("g", g, desc.g_type, desc.g_stride, desc.rows, desc.cols, desc.g_batch, desc.batch),
+              ("o", o, desc.o_type, desc.o_stride, desc.rows, desc.cols, desc.o_batch, desc.batch))
+    _fit(("workspace", workspace, None, 0))
     _check(_load().wino_orthogonalise(C.byref(desc), _ptr(g), _ptr(o), _ptr(workspace),
                                       _room(workspace), _stream(stream)))
     return o
