@@ -465,10 +465,11 @@ int wino_linear_cross_entropy(const wino_loss_desc_t* d, const void* h, const vo
  *   dl_tv = (exp(l_tv - lse_t) - [v = target_t]) dloss_t,
  *   dh = dl w,  dw = dl^T h,  dbias = sum_t dl
  * dh [rows][features] and dw [classes][features] dense, of `type`; dbias
- * [classes] fp32; each may be null.  Before the two products dl / max|dloss| is
- * rounded, for bf16 to bf16 (for 64 rows or fewer, and small products, to 16
- * bits), for fp32 like the other factors (dbias sums it unrounded).  Without rows dw and dbias
- * are zeros. */
+ * [classes] fp32; each may be null.  A dloss that is NaN or infinite makes its
+ * row of dh, dw and dbias NaN or infinite, and no other row of dh.  Before the
+ * two products dl / max|dloss|, over the finite ones, is rounded, for bf16 to
+ * bf16 (for 64 rows or fewer, and small products, to 16 bits), for fp32 like the
+ * other factors (dbias sums it unrounded).  Without rows dw and dbias are zeros. */
 int wino_linear_cross_entropy_backward_workspace_bytes(const wino_loss_desc_t* d, size_t* bytes);
 int wino_linear_cross_entropy_backward(const wino_loss_desc_t* d, const void* h, const void* w,
                                        const void* bias, const void* targets, const void* lse,

@@ -24,7 +24,7 @@
 // fp16 planes (22 bits) under one power of two for W and one for h (in the forward pass one a row, so that
 // no row's magnitude touches another's lse; of few rows and large W, or few classes and large h, fp32 as it stands, cut between
 // LDS and the matrix instructions: W is then read and nothing else); in the backward pass rows that are left out count as
-// zeros, whatever they hold, and do not enter the power of two.  dl is kept relative to the largest
+// zeros, whatever they hold, and do not enter the power of two.  dl is kept relative to the largest finite
 // |dloss|, by which the products' results are multiplied in fp32: with one weight for all rows, as
 // for a mean, the -1 of a target's class stays free of a rounding that would be the same in every row.
 #include "wino_products.hpp"
@@ -41,7 +41,7 @@ constexpr float kInf = __builtin_inff();
 
 // Numbers that kernels hand to later ones.
 struct Numbers {
-  float ref;              // largest |dloss|
+  float ref;              // largest finite |dloss|, one where that is zero
   int of_w, of_h;         // exponents of W's, h's planes: they hold 2^e times the values
   float max_w[kRange], max_h[kRange];
 };
@@ -99,7 +99,8 @@ __device__ __forceinline__ float range_of(const float* x, long ld, int rows, int
   return group_max(m, lds);
 }
 
-// First kernel of a backward pass: the largest |dloss| of the rows that count, and for fp32 the ranges of W and
+// First kernel of a backward pass: the largest finite |dloss| of the rows that count (a row whose dloss is NaN or
+// infinite keeps it in its dl / ref), and for fp32 the ranges of W and
 // of h's rows that count, or a copy of h in which the other rows are zeros.
 __global__ __launch_bounds__(1024) void k_loss_range(const float* __restrict__ w, long w_ld,
                                                      const float* __restrict__ h, long h_ld, int features, Rows g,
@@ -117,9 +118,9 @@ __global__ __launch_bounds__(1024) void k_loss_range(const float* __restrict__ w
   if (dloss && blockIdx.x == 0) {
     float m = 0;
     for (int t = threadIdx.x; t < g.rows; t += 1024)
-      if (g.kept(t)) m = __builtin_fmaxf(m, __builtin_fabsf(dloss[t]));
+      if (const float v = __builtin_fabsf(dloss[t]); v < kInf && g.kept(t)) m = __builtin_fmaxf(m, v);
     m = group_max(m, lds);
-    if (threadIdx.x == 0) to->ref = m;
+    if (threadIdx.x == 0) to->ref = m > 0 ? m : 1.f;
   }
   if (w) {
     const float m = range_of(w, w_ld, g.classes, features, nullptr, lds);
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
     to_logits<T>(g, v0, row, acc, j);
     const bool kept = t < g.g.rows && g.g.kept(row);
     const float all = kept ? lse[row] : 0.f;
-    float weight = kept && all != -kInf && scale != 0.f ? dloss[row] / scale : 0.f;
+    const float weight = kept && all != -kInf ? dloss[row] / scale : 0.f;
     const long off = kept ? g.g.target[row] - g.first - v0 : -1;
     const bool near = __any(off >= 0 && off < T::TM * 16);
 #pragma unroll
