@@ -56,8 +56,9 @@ int norm_args(const wino_norm_desc_t* d, NormArgs* a) {
   if (!std::isfinite(d->eps) || d->eps < 0) return refuse(WINO_EINVAL, "%s", "eps must be finite and not negative");
   if (d->y_type == WINO_TYPE_I8 && !positive(d->s_y))
     return refuse(WINO_EINVAL, "%s", "s_y must be positive and finite");
-  *a = NormArgs{(long)d->rows, d->channels, d->x_type, d->y_type, d->g_type, d->eps,
-                d->y_type == WINO_TYPE_I8 ? 1.0 / (double)d->s_y : 0.0, 1.0 / d->channels, 0, 0, 0, 0};
+  const double s = d->y_type == WINO_TYPE_I8 ? (double)d->s_y : 1.0;
+  *a = NormArgs{(long)d->rows, d->channels, d->x_type, d->y_type, d->g_type, d->eps, s, 1.0 / s,
+                1.0 / d->channels, 0, 0, 0, 0};
   if (int rc = stride_of(d->x_stride, d->channels, "x_stride", &a->x_stride)) return rc;
   if (int rc = stride_of(d->y_stride, d->channels, "y_stride", &a->y_stride)) return rc;
   if (int rc = stride_of(d->dy_stride, d->channels, "dy_stride", &a->dy_stride)) return rc;

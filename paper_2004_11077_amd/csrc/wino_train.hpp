@@ -15,7 +15,7 @@ struct NormArgs {
   long rows;
   int channels, x_type, y_type, g_type;
   float eps;
-  double inv_s, inv_c;    // 1 / s_y, 1 / channels
+  double s, inv_s, inv_c; // s_y, 1 / s_y, 1 / channels
   long x_stride, y_stride, dy_stride, dx_stride;
 };
 hipError_t launch_norm(const NormArgs& a, const void* x, const float* gamma, const float* beta, void* y,

@@ -1,0 +1,52 @@
+"""int8 codes on the border between two: rint(y / s_y) of the formula, ties to even.  y is exactly beta where a row
+has one value or gamma is zero, and (k + 1/2) s_y is exact in fp32 for s_y = n 2^-14 with few bits, so the
+quotient is a tie and nothing but the formula's own rounding decides."""
+import numpy as np
+import pytest
+
+from oracle import training as tr
+
+pytestmark = pytest.mark.gpu
+
+STEPS = [n * 2.0 ** -14 for n in (1, 3, 49, 99, 343, 1023, 1999)]
+
+
+def codes(x, gamma, beta, s_y, stride=0):
+    import torch
+    import paper_2004_11077_amd as wn
+    rows, channels = x.shape
+    cuda = lambda a: None if a is None else torch.from_numpy(np.asarray(a, np.float32)).cuda()
+    q = torch.full((rows, channels), 99, dtype=torch.int8, device="cuda")
+    t = cuda(x)
+    type = wn.TYPE_F32
+    if (t.to(torch.bfloat16).float() == t).all():
+        t, type = t.to(torch.bfloat16), wn.TYPE_BF16
+    wn.wino_layer_norm(wn.NormDesc(rows, channels, x_type=type, y_type=wn.TYPE_I8, s_y=s_y), t, cuda(gamma), cuda(beta), q)
+    return q.cpu().numpy()
+
+
+def borders(channels, s_y):
+    """(k + 1/2) s_y for all codes k, and two codes beyond them."""
+    k = np.resize(np.arange(-130, 130), channels)
+    return ((k + 0.5) * s_y).astype(np.float32)
+
+
+@pytest.mark.parametrize("s_y", STEPS)
+@pytest.mark.parametrize("channels", [255, 256, 20001])
+def test_channels_without_a_weight(channels, s_y):
+    rng = np.random.default_rng(channels)
+    beta = borders(channels, s_y)
+    got = codes(rng.standard_normal((5, channels)), np.zeros(channels), beta, s_y)
+    assert np.array_equal(got, np.broadcast_to(tr.codes(beta.astype(np.float64), s_y), got.shape))
+
+
+@pytest.mark.parametrize("channels", [96, 97, 20001])
+@pytest.mark.parametrize("s_y", [2.0 ** -149, 1e-30, 0.03, 3e38])
+def test_quotients_beyond_the_codes(channels, s_y):
+    """Infinities and the largest values stop at the last code, NaN gives 0."""
+    s_y = float(np.float32(s_y))
+    beta = np.resize(np.float32([np.inf, -np.inf, 3.4e38, -3.4e38, 1e-45, -1e-45, 0, np.nan, 1, -300]), channels)
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = np.clip(np.rint(beta.astype(np.float64) / s_y), -127, 127)
+    got = codes(np.full((2, channels), 5.0), None, beta, s_y)
+    assert np.array_equal(got, np.broadcast_to(np.nan_to_num(want).astype(np.int8), got.shape))
