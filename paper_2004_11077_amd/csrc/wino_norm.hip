@@ -147,6 +147,15 @@ __device__ __forceinline__ void codes_of(const double (&y)[VEC], double s, doubl
     }
 }
 
+// A row's mean, the correctly rounded quotient where the product with 1 / channels may be a last place off: a row of
+// one value whose sum is exact has that value as its mean and nothing left beside it, neither to be divided by the
+// root of eps nor to move a code off its border.
+template <class F>
+__device__ __forceinline__ F mean_of(F sum, const NormArgs& a) {
+  const F q = sum * (F)a.inv_c, left = __builtin_elementwise_fma(-q, (F)a.channels, sum);
+  return left == left ? __builtin_elementwise_fma(left, (F)a.inv_c, q) : q;   // an infinite sum leaves a NaN
+}
+
 // 1 / sqrt(v).  64 bits: the instruction's 26 bits and two steps of r <- r (3 - v r r) / 2.
 __device__ __forceinline__ float inverse_root(float v) { return 1.f / __builtin_sqrtf(v); }
 __device__ __forceinline__ double inverse_root(double v) {
@@ -182,7 +191,7 @@ __global__ __launch_bounds__(kThreads<LANES>) void k_norm(NormArgs a, const TI* 
 #pragma unroll
     for (int e = 0; e < VEC; ++e) sum += (F)v[i][e];
   }
-  const F mu = sum_lanes<LANES>(sum, lds) * (F)a.inv_c;
+  const F mu = mean_of(sum_lanes<LANES>(sum, lds), a);
   F sq = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -245,7 +254,7 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a, const TI* __rest
   const TI* px = x + row * a.x_stride;
   F sum = 0;
   for (int c = threadIdx.x; c < a.channels; c += 1024) sum += (F)widen(px[c]);
-  const F mu = sum_lanes<1024>(sum, lds) * (F)a.inv_c;
+  const F mu = mean_of(sum_lanes<1024>(sum, lds), a);
   F sq = 0;
   for (int c = threadIdx.x; c < a.channels; c += 1024) {
     const F d = (F)widen(px[c]) - mu;

@@ -50,3 +50,26 @@ def test_quotients_beyond_the_codes(channels, s_y):
         want = np.clip(np.rint(beta.astype(np.float64) / s_y), -127, 127)
     got = codes(np.full((2, channels), 5.0), None, beta, s_y)
     assert np.array_equal(got, np.broadcast_to(np.nan_to_num(want).astype(np.int8), got.shape))
+
+
+@pytest.mark.parametrize("s_y", STEPS)
+@pytest.mark.parametrize("channels", [49, 63, 255, 256, 520, 2049, 20001])
+def test_rows_of_one_value(channels, s_y):
+    beta = borders(channels, s_y)
+    assert (np.abs(beta.astype(np.float64) / s_y % 1) == 0.5).all()
+    for values in ([3.25, -1000.0, 0.0, 2.0 ** 60], [1 / 3, 1e5 + 0.1, -7e-5, 1e20]):     # exact in bf16; in fp32 alone
+        x = np.repeat(np.float32(values)[:, None], channels, 1)
+        got = codes(x, None, beta, s_y)
+        assert np.array_equal(got, np.broadcast_to(tr.codes(beta.astype(np.float64), s_y), got.shape)), values
+
+
+@pytest.mark.parametrize("channels", [49, 70, 96, 2047, 3001, 20000])
+def test_fp32_rows_of_one_value_are_beta(channels):
+    """The sum of a row is exact here, and so is the mean: nothing is left beside it."""
+    import torch
+    import paper_2004_11077_amd as wn
+    x = torch.tensor([1000.0, -3.0, 0.0, 96.5], device="cuda")[:, None].repeat(1, channels)
+    beta = torch.randn(channels, device="cuda")
+    y, mean = torch.empty_like(x), torch.empty(4, device="cuda")
+    wn.wino_layer_norm(wn.NormDesc(4, channels), x, None, beta, y, mean)
+    assert torch.equal(mean, x[:, 0]) and torch.equal(y, beta.expand_as(y))
