@@ -156,13 +156,14 @@ __device__ __forceinline__ F mean_of(F sum, const NormArgs& a) {
   return left == left ? __builtin_elementwise_fma(left, (F)a.inv_c, q) : q;   // an infinite sum leaves a NaN
 }
 
-// 1 / sqrt(v).  64 bits: the instruction's 26 bits and two steps of r <- r (3 - v r r) / 2.
+// 1 / sqrt(v).  64 bits: the instruction's 26 bits and two steps of r <- r (3 - v r r) / 2; of zero (a row of one value
+// and no eps) infinity, from which a step would make a NaN.
 __device__ __forceinline__ float inverse_root(float v) { return 1.f / __builtin_sqrtf(v); }
 __device__ __forceinline__ double inverse_root(double v) {
   double r = __builtin_amdgcn_rsq(v);
 #pragma unroll
   for (int i = 0; i < 2; ++i) r = r * __builtin_fma(-0.5 * v * r, r, 1.5);
-  return r;
+  return v == 0 ? __builtin_inf() : r;
 }
 
 template <class TI, class F, int LANES, int VEC, int NV>

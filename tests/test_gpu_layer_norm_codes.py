@@ -73,3 +73,23 @@ def test_fp32_rows_of_one_value_are_beta(channels):
     y, mean = torch.empty_like(x), torch.empty(4, device="cuda")
     wn.wino_layer_norm(wn.NormDesc(4, channels), x, None, beta, y, mean)
     assert torch.equal(mean, x[:, 0]) and torch.equal(y, beta.expand_as(y))
+
+
+@pytest.mark.parametrize("y_type", ["f32", "i8"])
+@pytest.mark.parametrize("channels", [64, 100, 3001, 20001])
+def test_rows_of_one_value_without_eps(channels, y_type):
+    """rstd is 1 / sqrt(0), infinity, whatever comes out; y is 0 times that, NaN, whose code is 0."""
+    import torch
+    import paper_2004_11077_amd as wn
+    x = torch.randn(4, channels, device="cuda")
+    x[1], x[2] = 2.5, 0
+    codes = y_type == "i8"
+    y = torch.full((4, channels), 9, device="cuda").to(torch.int8 if codes else torch.float32)
+    mean, rstd = torch.empty(2, 4, device="cuda")
+    wn.wino_layer_norm(wn.NormDesc(4, channels, y_type=wn.TYPE_I8 if codes else wn.TYPE_F32, s_y=0.02, eps=0), x, None, None, y, mean, rstd)
+    assert torch.isposinf(rstd[1:3]).all() and torch.isfinite(rstd[[0, 3]]).all()
+    assert mean[1] == 2.5 and mean[2] == 0
+    assert not y[1:3].any() if codes else torch.isnan(y[1:3]).all()
+    ref, _, rrstd = tr.layer_norm(x[[0, 3]].double().cpu().numpy(), 1.0, 0.0, 0.0)
+    if codes:
+        assert np.array_equal(y[[0, 3]].cpu().numpy(), tr.codes(ref, 0.02))
