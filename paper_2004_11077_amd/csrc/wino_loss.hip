@@ -34,17 +34,10 @@ namespace wino {
 namespace {
 
 using namespace prod;
+using namespace loss;
 
-constexpr int kRange = 256;        // partial maxima of a tensor
 constexpr int kDlExponent = 15;    // fp16 planes of dl: |dl| <= 1 relative to the largest |dloss|
 constexpr float kInf = __builtin_inff();
-
-// Numbers that kernels hand to later ones.
-struct Numbers {
-  float ref;              // largest finite |dloss|, one where that is zero
-  int of_w, of_h;         // exponents of W's, h's planes: they hold 2^e times the values
-  float max_w[kRange], max_h[kRange];
-};
 
 // exp(x) for x <= 0 or so by exp2; the argument's rounding is |x| 2^-24, which is most where exp is
 // least.
@@ -586,22 +579,6 @@ struct Tiles {
 // (A training step of 900 x 4092 x 401 in bf16: 104 us, all of ring 2 125; of 3 x 925 x 75113 in fp32: 328, all of
 // ring 4 428.)
 constexpr long kDeepGroups = 512;
-long count_of(long m, long n, long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
-// Products with k along the rows of both operands, over k of them: 32 x 32 with k shared by the waves where
-// there are few tiles, which for fp32, three or six products a term, are more, and more again where half
-// of a tile of 64 or more would be empty.  (Training steps: 64 x 512 x 2048 in fp32 56 us, with tiles of 64 62;
-// 4330 x 3610 x 8, 68 tiles: 178 and 251; 4096 x 2048 x 128, 128 tiles: 191 and 169; 3 x 925 x 10000, 157 tiles: 67
-// and 95; 900 x 4092 x 401 in bf16, 105 tiles: 128 and 104.)
-constexpr long few_tiles(bool bf16) { return bf16 ? 64 : 128; }
-int least_side(bool bf16, long m, long n, long k) {
-  const long few = !bf16 && (m <= 32 || n <= 32) ? 256 : few_tiles(bf16);
-  return count_of(m, n, 64) < few && k >= 256 ? 32 : 64;
-}
-int side_along(bool bf16, long m, long n, long k) {
-  const int side = side_for(m, n, 1);
-  return side == 64 ? least_side(bf16, m, n, k) : side;
-}
-constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
 
 template <int NP, bool AX, bool BX, class F>
 void with_tile(int side, long groups, F&& f) {
@@ -618,18 +595,6 @@ void with_tile(int side, long groups, F&& f) {
 // bf16 rows that the products can take where they lie: 16-byte accesses, whole stages of k.
 bool direct(const LossArgs& a, const void* p, long stride) {
   return a.bf16 && a.features % 64 == 0 && stride % 8 == 0 && stride <= kMaxLd && ((uintptr_t)p & 15) == 0;
-}
-
-// fp32 as it stands: few rows or classes, where the time is the passage of W or h through memory (75113 x 925 and 3 rows, a
-// training step: 326 us, by way of planes 821; 192 rows 907 and 1149, 256 rows 1160 and 1237; 256 x 1024 x
-// 8192, where every tile of W is cut four times: 151 and 143; 44 x 1452 x 2481: 70 and 97; 20000 x 1030 x 3: 228 and 299; 4096 x 2048 x 128: 197 and 169).  Values below 2^-102
-// lose lower pieces to bf16's smallest numbers there, which planes keep, so small tensors, where the gain is
-// a few microseconds of launches (64 x 64 x 1000: 42.3 us and 45.2), stay with the planes.
-bool as_it_stands(const LossArgs& a) {
-  const double least = 1 << 16;
-  return !a.bf16 && a.h_stride <= kMaxLd / 2 && a.w_stride <= kMaxLd / 2 &&
-         ((a.rows <= 192 && (double)a.features * a.classes >= least) ||
-          (a.classes <= 64 && (double)a.features * a.rows >= least));
 }
 
 const void* row_at(const LossArgs& a, const void* p, long row, long stride) {
@@ -691,7 +656,7 @@ hipError_t forward(const LossArgs& a, const void* h, const void* w, const float*
     q.count = (int)(a.classes - first < piece ? a.classes - first : piece);
     operands<NP>(a, l, g, row_at(a, w, first, a.w_stride), q.count, h, w_direct, h_ready, false, num, ws, &ow, &oh, st);
     h_ready = true;
-    with_tile<NP, false, false>(NP == 3 ? least_side(false, q.count, a.rows, l.dp) : side_along(a.bf16, q.count, a.rows, l.dp),
+    with_tile<NP, false, false>(logits_side(a, l, q.count),
                                 count_of(q.count, a.rows, 64), [&](auto tile) {
       typedef decltype(tile) T;
       const int tm = (q.count + T::BM - 1) / T::BM, tn = (a.rows + T::BN - 1) / T::BN;
@@ -756,9 +721,9 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
                      a.rows, a.features, ref, &num->of_w};
     const Product pw{od, oh, rest, dw_sums ? (void*)dw_sums : dw_rows, dw_items, dw_sums ? 2 : a.bf16, tk, dw_per, q.count,
                      a.features, ref, &num->of_h};
-    const int dw_side = dw_sums || NP == 3 ? 64 : side_for(q.count, a.features, 1);
+    const int side_w = dw_side(a, l, q.count);
     const auto tiles = [](const Product& p, int side) { return (int)count_of(p.count, p.width, side); };
-    if (dh && dw && l.dh_side == 64 && dw_side == 64) {
+    if (dh && dw && l.dh_side == 64 && side_w == 64) {
       const int th = tiles(ph, 64), tw = tiles(pw, 64), all = th * l.splits;
       const auto launch = [&](auto h, auto w) {
         typedef decltype(h) H;
@@ -784,8 +749,8 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
       else if (dh)
         with_tile<NP, false, true>(l.dh_side, groups_h, [&](auto t) { launch(t, std::false_type{}, ph, l.splits); });
       if (dw)
-        with_tile<NP, true, true>(dw_side, groups_w, [&](auto t) {
-          if (whole(pw, dw_side)) launch(t, std::true_type{}, pw, l.dw_splits);
+        with_tile<NP, true, true>(side_w, groups_w, [&](auto t) {
+          if (whole(pw, side_w)) launch(t, std::true_type{}, pw, l.dw_splits);
           else launch(t, std::false_type{}, pw, l.dw_splits);
         });
     }
@@ -804,68 +769,6 @@ hipError_t backward(const LossArgs& a, const void* h, const void* w, const float
 }
 
 }  // namespace
-
-LossLayout loss_layout(const LossArgs& a, bool back) {
-  LossLayout l{};
-  const size_t T = (size_t)a.rows, D = (size_t)a.features, V = (size_t)a.classes;
-  const int np = a.bf16 ? 1 : 2;
-  const size_t item = 2 * (size_t)np;   // bytes of a value in planes
-  l.dp = (int)up(D, 64);
-  // classes per piece: what the caller asks for, or as many as keep a piece's dl, and its planes of W if
-  // it may need them, within 256 MiB
-  const size_t most = T > (size_t)l.dp || as_it_stands(a) ? T : (size_t)l.dp;
-  size_t piece = a.piece ? (size_t)a.piece : ((size_t)256 << 20) / (item * (most ? most : 1));
-  piece = up(piece < 1024 && !a.piece ? 1024 : piece, 256);
-  if (piece > (size_t)kMaxLd / 2) piece = (size_t)kMaxLd / 2;   // rows of dl on two planes
-  l.piece = (int)(piece < V ? piece : V);
-  const size_t P = (size_t)l.piece, vp = up(P, 64);
-  size_t at = 0;
-  const auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
-  l.numbers = take(sizeof(Numbers));
-  if (!as_it_stands(a)) l.w = take(item * P * l.dp);
-  l.h = take(item * T * l.dp);
-  l.splits = 1;
-  if (!back) {
-    // pieces are whole multiples of 256 classes, so no tile spans two
-    // of side_along() for any classes (32 or fewer are one tile of either side)
-    const size_t least = T >= 64 * (size_t)few_tiles(a.bf16) ? 64 : 32;
-    l.parts = take(8 * T * (up(V, 256) / least));
-    l.target = take(4 * T);
-    l.unit_w = take(4 * P);
-    l.unit_h = take(4 * T);
-  } else {
-    l.dl = take(item * T * vp);
-    // bf16: dl's rounding averages out over many rows; with few of them, or little to do, it is kept on
-    // two bf16 values
-    l.two = a.bf16 && (T <= 64 || (double)T * D * V <= 1 << 30);
-    if (l.two) l.rest = take(item * T * vp);
-    const bool stands = as_it_stands(a);
-    l.side = stands ? least_side(false, (long)P, (long)T, l.dp) : side_along(a.bf16, (long)P, (long)T, l.dp);
-    // ranges of classes, each of 512 or more, until dh's tiles fill the chip: one tile of 256 a compute
-    // unit, or two of the smaller ones
-    const long room = (long)(vp / 512 ? vp / 512 : 1);
-    double most = 0;
-    for (int side = stands ? 64 : 256; side >= 64 && T; side /= 2) {
-      const long tiles = count_of((long)D, (long)T, side), slots = side == 256 ? 256 : 512;
-      long ranges = slots / tiles;
-      ranges = ranges > room ? room : ranges < 1 ? 1 : ranges;
-      const double score = rate_of(side) * D * T * ranges / ((double)((tiles * ranges + 255) / 256) * 256 * side * side);
-      if (score > most) most = score, l.dh_side = side, l.splits = (int)ranges;
-    }
-    if (l.splits > 64) l.splits = 64;   // k_loss_sums adds them up one after the other
-    l.dh = take(4 * T * D * l.splits);
-    // ranges of rows, each of 256 or more, where dW has few tiles of 64 (a training step of 2048 x 64 x 1000 in
-    // fp32: 63 us, without them 87)
-    const long tiles = count_of((long)P, (long)D, 64);
-    long ranges = tiles < 128 ? 256 / tiles : 1;
-    if (ranges > (long)T / 256) ranges = (long)T / 256;
-    l.dw_splits = (int)(ranges < 1 ? 1 : ranges > 64 ? 64 : ranges);
-    if (l.dw_splits > 1) l.dw = take(4 * P * D * l.dw_splits);
-    l.dbias = take(4 * V * waves_n(l.side) * (T ? (T + l.side - 1) / l.side : 1));
-  }
-  l.bytes = at;
-  return l;
-}
 
 hipError_t launch_loss(const LossArgs& a, const void* h, const void* w, const float* bias,
                        const int64_t* target, float* loss, float* lse, char* ws, hipStream_t st) {

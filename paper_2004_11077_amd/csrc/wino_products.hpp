@@ -41,6 +41,7 @@
 
 #include "wino_kernels.hpp"
 #include "wino_product_sources.hpp"
+#include "wino_train_rules.hpp"
 
 namespace wino {
 namespace prod {
@@ -53,8 +54,6 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-
-constexpr long kMaxLd = 1L << 21;   // elements between rows: 256 rows of it are 2^30 bytes
 
 // One operand: `rows` rows of `cols` elements, batch b, row r at p + b batch + r ld, element e of plane q
 // there at place<NP>(e) + 32 q; fp32 (NP = 3): at 2 e, strides in 16-bit units too.  k along the rows: m or n is r, k is e.  Across: k is r, m or n is e.
@@ -112,25 +111,6 @@ __device__ __forceinline__ f32x4 multiply_block(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Share of the 256 x 256 tiles' rate that other tiles reach when nothing is idle (16384 x 2048 x 4096 in bf16:
-// 1421 TFLOP/s and 1297; two planes, 13824 x 512 x 512: 128 x 128 tiles 22.2 us with 0.84 of the chip at work,
-// 64 x 64 ones 25.6 us with 0.96).
-inline double rate_of(int side) { return side == 256 ? 1.0 : side == 128 ? 0.92 : 0.8; }
-// Side of the square tiles (256, 128 or 64) for `z` products of m x n: the one that leaves least of the
-// chip idle, counting what of its tiles lies outside, and compute units that wait for the others' last tile.
-// (X of 6144 x 1536, k of 1536: 128 x 128 tiles 130 us, 64 x 64 ones 123; of 3 x 4608 x 512, k of 512: 33.5
-// and 39.)
-inline int side_for(double m, double n, double z) {
-  int best = 64;
-  double most = 0;
-  for (int side = 256; side >= 64; side /= 2) {
-    const double tiles = __builtin_ceil(m / side) * __builtin_ceil(n / side) * z;
-    const double score = rate_of(side) * m * n * z / (__builtin_ceil(tiles / 256) * 256 * side * side);
-    if (score > most) most = score, best = side;
-  }
-  return best;
 }
 
 // Work group of a grid of `all` -> its place.  Consecutive work groups go round robin over the 8 XCDs;

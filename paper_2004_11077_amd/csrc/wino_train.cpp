@@ -3,7 +3,7 @@
 
 #include "../../include/wino.h"
 #include "wino_kernels.hpp"
-#include "wino_train.hpp"
+#include "wino_train_rules.hpp"
 
 using namespace wino;
 

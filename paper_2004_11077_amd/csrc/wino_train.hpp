@@ -43,7 +43,6 @@ struct LossLayout {
   int two;                // bf16: dl on two values
   size_t numbers, w, h, parts, target, unit_w, unit_h, dl, rest, dh, dw, dbias, bytes;
 };
-LossLayout loss_layout(const LossArgs& a, bool backward);
 hipError_t launch_loss(const LossArgs& a, const void* h, const void* w, const float* bias,
                        const int64_t* target, float* loss, float* lse, char* ws, hipStream_t st);
 hipError_t launch_loss_backward(const LossArgs& a, const void* h, const void* w, const float* bias,
@@ -61,7 +60,6 @@ struct UpdateLayout {
   int side, splits;           // tiles and ranges of k of A's product
   size_t norms, x, x2, gram, poly, parts, bytes;
 };
-UpdateLayout update_layout(const UpdateArgs& a);
 hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, hipStream_t st);
 
 }  // namespace wino

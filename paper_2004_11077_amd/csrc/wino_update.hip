@@ -25,8 +25,7 @@ namespace wino {
 namespace {
 
 using namespace prod;
-
-constexpr int kNormParts = 256;
+using namespace update;
 
 __device__ __forceinline__ float value(const void* p, long i, int bf16) {
   return bf16 ? bf16_value(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
@@ -275,13 +274,6 @@ struct Tiles {
   typedef Tile<64, 64, 2, 2, 2, 4, AX> Deep;   // where two work groups a compute unit are all there are
 };
 
-int tiles_of(int side, int tile) { return (side + tile - 1) / tile; }
-int half_of(int tiles) { return tiles * (tiles + 1) / 2; }
-
-// Symmetric products of few tiles and not many k: no barriers, one launch.  (A of 4 x 64 rows, k of 576: 8.4
-// us, and 9.5 in four ranges with their join; of 3 x 256 rows, k of 2304: 20.9 us and 18.9.)
-bool few(const UpdateLayout& l, int batch, int k) { return (long)l.r * l.r * batch <= 256L * 256 * 4 && k <= 1024; }
-
 template <Kind KIND>
 void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& y, int k, const Result& s,
              float* parts, hipStream_t st) {
@@ -315,7 +307,7 @@ void product(const UpdateLayout& l, int batch, const Operand& x, const Operand& 
       wino_launch((k_update_product<T, KIND>), dim3(tm * tn * batch), dim3(T::THREADS), st, x, y, k, k, tm * tn, tm,
                   s, (float*)nullptr, 0L, 0);
     };
-    const int side = side_for(l.c, l.r, batch);
+    const int side = next_side(l, batch);
     if (side == 256) go(Tiles<true>::Big{});
     else if (side == 128) go(Tiles<true>::Mid{});
     else if ((long)tiles_of(l.c, 64) * tiles_of(l.r, 64) * batch <= 512) go(Tiles<true>::Deep{});
@@ -333,34 +325,6 @@ int exponent(double most) {
 }
 
 }  // namespace
-
-UpdateLayout update_layout(const UpdateArgs& a) {
-  UpdateLayout l{};
-  l.r = a.rows < a.cols ? a.rows : a.cols;
-  l.c = a.rows < a.cols ? a.cols : a.rows;
-  l.rp = (int)up(l.r, 64);
-  l.cp = (int)up(l.c, 64);
-  size_t at = 0;
-  const auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
-  const size_t item = 2 * 2 * (size_t)a.batch;   // two planes
-  l.norms = take(sizeof(double) * kNormParts * a.batch);
-  l.x = take(item * l.r * l.cp);
-  l.x2 = take(item * l.r * l.cp);
-  l.gram = take(item * l.r * l.rp);
-  l.poly = take(item * l.r * l.rp);
-  l.splits = 1;
-  if (a.batch && l.r && !few(l, a.batch, (int)up(l.c, 32))) {
-    // ranges of A's k until its tiles fill the chip, each of 512 or more
-    l.side = (long)half_of(tiles_of(l.r, 128)) * a.batch >= 64 ? 128 : 64;
-    const long tiles = (long)half_of(tiles_of(l.r, l.side)) * a.batch;
-    long s = (512 + tiles / 2) / tiles;
-    if (s > l.cp / 512) s = l.cp / 512;
-    l.splits = (int)(s < 1 ? 1 : s);
-    if (l.splits > 1) l.parts = take(4 * (size_t)l.splits * a.batch * l.r * l.rp);
-  }
-  l.bytes = at ? at : 256;
-  return l;
-}
 
 hipError_t launch_update(const UpdateArgs& a, const void* g, void* o, char* ws, hipStream_t st) {
   const UpdateLayout l = update_layout(a);
