@@ -611,6 +611,9 @@ def _reach(*tensors):
         if t is None or rows < 1 or row < 1 or count < 1:
             continue
         whole = t.is_contiguous()
+        if not whole and t.dim() == 4 and t.shape[1] == row and t.stride(1) == 1:
+            t = t.permute(0, 2, 3, 1)       # [N][C][H][W] with the channels last in memory: rows of channels
+            whole = t.is_contiguous()
         if not (stride or batch):
             if not whole:
                 raise WinoError(-1, "%s is not contiguous, and the descriptor has no stride for it" % name)
@@ -684,10 +687,10 @@ def wino_linear_cross_entropy_backward(desc, h, w, bias, targets, lse, dloss, dh
                                        workspace, stream=None):
     """Gradients of wino_linear_cross_entropy; each of dh, dw and dbias may be None."""
     t, d, v = desc.rows, desc.features, desc.classes
-    _fit_rows(("h", h, desc.type, desc.h_stride, t, d), ("w", w, desc.type, desc.w_stride, v if t else 0, d))
+    _fit_rows(("h", h, desc.type, desc.h_stride, t, d), ("w", w, desc.type, desc.w_stride, v if t else 0, d),
+              ("dh", dh, desc.type, 0, t, d), ("dw", dw, desc.type, 0, v, d))
     _fit(("bias", bias, TYPE_F32, v), ("targets", targets, "i64", t), ("lse", lse, TYPE_F32, t),
-         ("dloss", dloss, TYPE_F32, t), ("dh", dh, desc.type, t * d), ("dw", dw, desc.type, v * d),
-         ("dbias", dbias, TYPE_F32, v), ("workspace", workspace, None, 0))
+         ("dloss", dloss, TYPE_F32, t), ("dbias", dbias, TYPE_F32, v), ("workspace", workspace, None, 0))
     _check(_load().wino_linear_cross_entropy_backward(
         C.byref(desc), _ptr(h), _ptr(w), _ptr(bias), _ptr(targets), _ptr(lse), _ptr(dloss),
         _ptr(dh), _ptr(dw), _ptr(dbias), _ptr(workspace), _room(workspace), _stream(stream)))
@@ -700,8 +703,12 @@ def wino_orthogonalise_workspace_bytes(desc):
 
 def wino_orthogonalise(desc, g, o, workspace, stream=None):
     """Orthogonalised updates of a batch of weight gradients."""
-    _fit_rows(("g", g, desc.g_type, desc.g_stride, desc.rows, desc.cols, desc.g_batch, desc.batch),
-              ("o", o, desc.o_type, desc.o_stride, desc.rows, desc.cols, desc.o_batch, desc.batch))
+    fit = g, o
+    if g is not None and o is not None and g.dim() == 4 and not g.is_contiguous() and g.stride() == o.stride():
+        # filters with their channels last in memory, alike in both: the columns' order changes nothing else
+        fit = g.permute(0, 2, 3, 1), o.permute(0, 2, 3, 1)
+    _fit_rows(("g", fit[0], desc.g_type, desc.g_stride, desc.rows, desc.cols, desc.g_batch, desc.batch),
+              ("o", fit[1], desc.o_type, desc.o_stride, desc.rows, desc.cols, desc.o_batch, desc.batch))
     _fit(("workspace", workspace, None, 0))
     _check(_load().wino_orthogonalise(C.byref(desc), _ptr(g), _ptr(o), _ptr(workspace),
                                       _room(workspace), _stream(stream)))

@@ -152,3 +152,30 @@ def test_tensors_that_lie_as_they_should():
     for bad in (("short", f(C - 1), F, C), ("type", f(C, dtype=torch.bfloat16), F, C)):
         with pytest.raises(wn.WinoError):
             binding._fit(bad)
+
+
+def test_channels_last_in_memory():
+    """[N][C][H][W] with the channels last in memory is [N][H][W][C]."""
+    F, last = wn.TYPE_F32, torch.channels_last
+    x = torch.zeros(2, 7, 3, 4).to(memory_format=last)
+    assert not x.is_contiguous()
+    binding._fit_rows(("dense", x, F, 0, 24, 7), ("some of them", torch.zeros(2, 10, 3, 4).to(memory_format=last)[:, :7], F, 10, 24, 7))
+    for bad in (("rows of others", x, F, 0, 42, 4), ("apart", x, F, 10, 24, 7), ("first", torch.zeros(2, 4, 7, 3).permute(0, 2, 3, 1), F, 0, 24, 7),
+                ("some", torch.zeros(2, 10, 3, 4).to(memory_format=last)[:, :7], F, 0, 24, 7)):
+        with pytest.raises(wn.WinoError):
+            binding._fit_rows(bad)
+
+
+def test_filters_with_channels_last_in_memory(monkeypatch):
+    """One order of the columns in both is as good as another; in one of them alone it is not."""
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: 0
+    d = wn.OrthogonaliseDesc(1, R, 9 * C)
+    last = f(R, C, 3, 3).to(memory_format=torch.channels_last)
+    refused(update, "g", last, o=f(R, C, 3, 3), desc=d)
+    refused(update, "o", last, g=f(R, C, 3, 3), desc=d)
+    refused(update, "g", f(C, R, 3, 3).transpose(0, 1), o=f(C, R, 3, 3).transpose(0, 1), desc=d)
+    monkeypatch.setattr(binding, "_load", Library)
+    update(g=last, o=torch.empty_like(last), desc=d)
+    update(g=f(R, C, 3, 3), o=f(R, C, 3, 3), desc=d)
