@@ -440,9 +440,10 @@ int wino_layer_norm_backward(const wino_norm_desc_t* d, const void* dy, const vo
  * targets [rows] int64, loss and lse [rows] fp32.  The logits are never kept:
  * they are computed in pieces and computed again in the backward pass.  A row
  * whose target is ignore_index or no class (below 0, classes or above) is left
- * out: loss 0, no gradient, whatever h holds there; its lse is still that of h.  Classes may
- * be masked by a bias of -infinity: a masked target's loss is +infinity; a row
- * with every class masked has lse -infinity, loss +infinity and no gradient.
+ * out: loss 0, no gradient, whatever h holds there; its lse is still that of h.
+ * Classes may be masked by a bias of -infinity, whatever finite values their
+ * weights hold: a masked target's loss is +infinity; a row with every class
+ * masked has lse -infinity, loss +infinity and no gradient.
  * Products of fp32 operands take 22 bits of each factor (of values below 2^-18
  * of the tensor's largest: 2^-39 of that), for 192 rows or fewer and 2^16 weights
  * or more, and for 64 classes or fewer and 2^16 values of h or more, 24 bits (of
