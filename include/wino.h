@@ -454,8 +454,9 @@ typedef struct {
   int type;                  /* of h, w, dh, dw                                 */
   int64_t h_stride, w_stride;
   int64_t ignore_index;
-  int piece;                 /* classes per piece, 0 = chosen by the library (about
-                                256 MiB of workspace); at most WINO_LOSS_MAX_ROWS */
+  int piece;                 /* classes per piece, 0 = chosen by the library (its dl
+                                and its copy of W take about 256 MiB each); at
+                                most WINO_LOSS_MAX_ROWS                         */
 } wino_loss_desc_t;
 int wino_linear_cross_entropy_workspace_bytes(const wino_loss_desc_t* d, size_t* bytes);
 int wino_linear_cross_entropy(const wino_loss_desc_t* d, const void* h, const void* w,
@@ -470,7 +471,14 @@ int wino_linear_cross_entropy(const wino_loss_desc_t* d, const void* h, const vo
  * row of dh, dw and dbias NaN or infinite, and no other row of dh.  Before the
  * two products dl / max|dloss|, over the finite ones, is rounded, for bf16 to
  * bf16 (for 64 rows or fewer, and small products, to 16 bits), for fp32 like the
- * other factors (dbias sums it unrounded).  Without rows dw and dbias are zeros. */
+ * other factors (dbias sums it unrounded): where those take 22 bits, to steps of
+ * 2^-39 at the finest, so that what is 2^-33 of the largest |dloss|, as the
+ * gradient of a class of probability 1e-10 or of a row whose dloss is that small
+ * beside another's, keeps six bits in dh and dw.  Without rows dw and dbias are
+ * zeros.  Besides a piece's dl and its copy of W the workspaces hold a copy of h,
+ * in the forward pass 8 bytes for every row and every 32 or 64 classes, in the
+ * backward pass fp32 sums of dh, of dw where it has few tiles, and 8 or 16 bytes
+ * for every class and tile of 32 to 256 rows. */
 int wino_linear_cross_entropy_backward_workspace_bytes(const wino_loss_desc_t* d, size_t* bytes);
 int wino_linear_cross_entropy_backward(const wino_loss_desc_t* d, const void* h, const void* w,
                                        const void* bias, const void* targets, const void* lse,

@@ -4,11 +4,11 @@
 //   dl_tv = (exp(l_tv - lse_t) - [v = target_t]) dloss_t,  dh = dl W,  dW = dl^T h,  db = sum_t dl
 //
 // What bounds it: the matrix pipe, 8 T D V operations for a training step of T rows, D features and V
-// classes (the logits are computed twice).  T = 4096, D = 2048, V = 65536 in bf16: 4.0 ms, 1.1 PFLOP/s, the
-// library's large product at 8192^3 reaching 1.3; 1001 x 515 x 10007 in fp32 on two planes: 266 us, 155
-// TFLOP/s of fp32 (465 of the matrix pipe's, tiles that are not full and the planes' copies are the rest).
+// classes (the logits are computed twice).  T = 4096, D = 2048, V = 65536 in bf16: 4.1 ms, 1.07 PFLOP/s, the
+// library's large product at 8192^3 reaching 1.3; 1001 x 515 x 10007 in fp32 on two planes: 270 us, 153
+// TFLOP/s of fp32 (459 of the matrix pipe's, tiles that are not full and the planes' copies are the rest).
 // Few rows: the weights' passage through memory.  One row of 4096 x 131072 in bf16: 176 us, 6.1 TB/s; a
-// training step of 3 x 925 x 75113 in fp32: 326 us, of which 160 read W and write dW.  Small ones: launches,
+// training step of 3 x 925 x 75113 in fp32: 324 us, of which 160 read W and write dW.  Small ones: launches,
 // 256 x 512 x 10: five in 33 us.
 //
 // Forward: the logits of a tile leave the matrix instructions in registers and end there as a maximum
@@ -482,8 +482,9 @@ __global__ __launch_bounds__(T::THREADS) void k_loss_dlogits(Operand w, Operand 
 // kind 0: to fp32, 1: to bf16, both times ref; 2: to fp32 sums of a range of k (blockIdx.y), kept as
 // they are, 3: added to what is there.  A lane of the instruction's result holds four consecutive m of
 // one n.  FOUR: m are the features, four of them one store (rows of out start on whole fours); otherwise
-// m are the rows, and sixteen lanes store neighbouring features.  (dW of 65536 x 2048 in bf16: 585 us and
-// 640; of 10007 x 515 in fp32, whose rows start anywhere: 60 and 55.)
+// m are the rows, and sixteen lanes store neighbouring features.  (dW of 2048 x 1024 x 16384 in bf16: 71 us and 78,
+// of a piece of 4096 x 2048 x 32768 574 and 580, of 4096 x 2048 x 8192 in fp32 326 and 329; dh there 84 and 84, 538 and
+// 531, 349 and 349; dW of 10007 x 515 in fp32, whose rows start anywhere: 60 and 55.)
 struct Product {
   Operand rows, features;
   const uint16_t* rest;  // of `rows`, may be null: a second product on top of the first

@@ -4,10 +4,11 @@
 //   xh = (x - mu) s, g = dy gamma:  dx = s (g - mean(g) - xh mean(g xh)),
 //   dgamma = sum_rows dy xh,  dbeta = sum_rows dy
 //
-// What bounds it is memory: each tensor passes once.  131072 x 64 fp32 to codes, 42.5 MB: 12.8 us, 3.4 TB/s
-// (the copy of a large tensor reaches 4.86); backward 16384 x 256 fp32, 50.4 MB: 13.6 us, 3.7 TB/s, of which
-// 3.9 us are the second launch that joins the columns' sums; 8192 x 4096 bf16, 201 MB: 53.8 us, 3.7 TB/s.
-// 64 x 16: 2.3 us, a launch.
+// What bounds it is memory: each tensor passes once.  8192 x 4096 fp32, 268 MB: 50.4 us, 5.3 TB/s (the copy of a
+// large tensor reaches 4.86), bf16, 134 MB: 32.5 us; backward 16384 x 256 fp32, 50.4 MB: 13.7 us, 3.7 TB/s, of
+// which 3.4 to 3.8 us are the second launch that joins the columns' sums; 8192 x 4096 bf16, 201 MB: 53.7 us, 3.7
+// TB/s.  Codes wait for their 64-bit arithmetic as well: 131072 x 64 fp32 to codes, 42.5 MB, takes 13.4 us, to bf16,
+// 50 MB, 11.7, to fp32, 67 MB, 13.7.  64 x 16: 2.2 us, a launch.
 //
 // A row is read once and stays in registers between its sums: LANES lanes hold it, NV vectors of VEC
 // values each.  The variance is the sum of squared differences from the mean, never a difference of

@@ -60,7 +60,7 @@ inline int side_along(bool bf16, long m, long n, long k) {
 constexpr int waves_n(int side) { return side == 256 ? 4 : 2; }
 
 // fp32 as it stands: few rows or classes, where the time is the passage of W or h through memory (75113 x 925 and 3 rows, a
-// training step: 326 us, by way of planes 821; 192 rows 907 and 1149, 256 rows 1160 and 1237; 256 x 1024 x
+// training step: 324 us, by way of planes 821; 192 rows 907 and 1149, 256 rows 1160 and 1237; 256 x 1024 x
 // 8192, where every tile of W is cut four times: 151 and 143; 44 x 1452 x 2481: 70 and 97; 20000 x 1030 x 3: 228 and 299; 4096 x 2048 x 128: 197 and 169).  Values below 2^-102
 // lose lower pieces to bf16's smallest numbers there, which planes keep, so small tensors, where the gain is
 // a few microseconds of launches (64 x 64 x 1000: 42.3 us and 45.2), stay with the planes.

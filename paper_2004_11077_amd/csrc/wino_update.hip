@@ -9,9 +9,9 @@
 // 3.4^4 in all for the usual coefficients, so bf16 results need the second plane as well.
 //
 // What bounds it: the matrix pipe for large matrices, launches for small ones, of which there are three or
-// four a step.  6144 x 1536: 1.07 ms where the 236 GFLOP of fp32 products need 0.54 at the rate of the
-// library's large bf16 product over three; 3 x 512 x 4608, bf16: 366 us for 0.13 ms of products; 3 x 256 x
-// 2304: 152 us; 4 x 64 x 576: 92 us for 17 launches.
+// four a step.  6144 x 1536: 1.09 ms where the 236 GFLOP of fp32 products need 0.54 at the rate of the
+// library's large bf16 product over three; 3 x 512 x 4608, bf16: 368 us for 0.13 ms of products; 3 x 256 x
+// 2304: 153 us; 4 x 64 x 576: 92 us for 17 launches.
 //
 // Powers of two that bring X, A and P into fp16's range are known on the host: no singular value of X
 // exceeds one at first, nor, after a step, the largest |a s + b s^3 + c s^5| of those before it, and no
