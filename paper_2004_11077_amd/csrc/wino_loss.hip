@@ -275,8 +275,12 @@ __device__ __forceinline__ void to_logits(const Logits& g, int v0, int j_t, f32x
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int v = v0 + i * 16 + e;
-        if (v >= g.count) acc[i][j][e] = -kInf;
-        else if (g.bias) acc[i][j][e] += g.bias[g.first + v];
+        if (v >= g.count) {
+          acc[i][j][e] = -kInf;
+        } else if (g.bias) {
+          const float b = g.bias[g.first + v];
+          acc[i][j][e] = b == -kInf ? b : acc[i][j][e] + b;   // also where the product overflows
+        }
       }
   }
 }

@@ -46,3 +46,22 @@ def test_masked_targets(T, D, V, type, piece):
     k = (r["target"] >= 0) & (r["target"] < V)
     assert np.isposinf(r["loss"][k & (r["target"] % 2 == 0)]).all() and (k & (r["target"] % 2 == 0)).any()
     check(r, type)
+
+
+@pytest.mark.parametrize("T,D,V,type,piece", SHAPES)
+def test_products_that_overflow(T, D, V, type, piece):
+    """A masked class's logit is -infinity also where h times its weights is +infinity."""
+    masked = np.r_[0:V // 3, V - 1]
+
+    def change(v):
+        def f(h, w, b, target, dloss):
+            b[masked] = -np.inf
+            target[np.isin(target, masked)] = V // 2
+            h.abs_()
+            for i in masked:
+                w[int(i)] = v
+        return f
+    got, zero = (run(T, D, V, type, piece=piece, change=change(v)) for v in (3.3e38, 0))
+    for name in ("loss", "lse", "dh", "dw", "dbias"):
+        assert np.array_equal(got[name], zero[name]), name
+    check(zero, type)
