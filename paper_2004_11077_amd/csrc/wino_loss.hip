@@ -18,9 +18,9 @@
 // (wino_products.hpp), so none of them is transposed in memory.
 //
 // bf16 operands are taken where they lie if their rows are whole pieces of 16 bytes and whole lines, and
-// from a padded copy otherwise; dl is rounded to bf16 like the gradients (of few rows, whose roundings do
-// not average out, or small products to two bf16 values: one row of two classes was off by 0.004 of the
-// gradient, twice a bf16 result's rounding).  fp32 operands become two
+// from a padded copy otherwise; dl is rounded to bf16 like the gradients, which then are off by 1.66e-3 to 2.06e-3
+// of their 2-norm where rounding the exact ones costs 1.66e-3 (of few rows or small products to two bf16 values, where
+// that costs little: one row of two classes was off by 0.004 of the gradient, twice a bf16 result's rounding).  fp32 operands become two
 // fp16 planes (22 bits) under one power of two for W and one for h (in the forward pass one a row, so that
 // no row's magnitude touches another's lse; of few rows and large W, or few classes and large h, fp32 as it stands, cut between
 // LDS and the matrix instructions: W is then read and nothing else); in the backward pass rows that are left out count as

@@ -112,8 +112,8 @@ inline LossLayout loss_layout(const LossArgs& a, bool back) {
     l.unit_h = take(4 * T);
   } else {
     l.dl = take(item * T * vp);
-    // bf16: dl's rounding averages out over many rows; with few of them, or little to do, it is kept on
-    // two bf16 values
+    // bf16: with few rows a gradient may be one term of dl, whose rounding is then as large as the result's; with
+    // few of them, or little to do, dl is kept on two bf16 values
     l.two = a.bf16 && (T <= 64 || (double)T * D * V <= 1 << 30);
     if (l.two) l.rest = take(item * T * vp);
     const bool stands = as_it_stands(a);
